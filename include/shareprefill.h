@@ -390,6 +390,153 @@ sp_status sp_prefill_layer_dict(const sp_shape *shape, const void *q, const void
                                 float *dist, int32_t *vs_idx, int32_t *vs_cnt, void *workspace, size_t workspace_bytes,
                                 void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * The paged key/value cache: what a served prompt needs next to its prefill.
+ *
+ * A cache holds `n_pages` pages of `page_size` tokens, per token n_kv_heads rows of head_dim keys and as many values, bf16, in
+ * two buffers of one geometry.  Slot s of the cache is token s % page_size of page s / page_size.  Row r of a block table
+ * (device int32 [n_requests][max_pages]) lists the pages of request r in order: its token at position p lies in page
+ * block_table[r][p / page_size].  A request holds `n_held` pages and its first ctx_len tokens are in the cache (its context).
+ *
+ * A step adds new tokens to every request: one, a chain, or a tree of drafted tokens of which later some are accepted.
+ *   sp_cache_plan     gives them pages, slots, positions and ancestors
+ *   sp_qk_norm_rope   per layer: norms and rotation of queries and keys; keys and values go to their slots
+ *   sp_cache_attn     per layer: attention of the new tokens over context and ancestors
+ *   sp_cache_accept   moves the accepted tokens' rows up behind the context
+ * The new tokens of all requests are packed: request r's are rows tok_start[r] .. tok_start[r + 1] of q, k, v and o; new token
+ * j of r lies at position ctx_len[r] + j of the cache, wherever it hangs in its tree.
+ *
+ * Everything that depends on lengths is read on the device, so a captured step replays with other lengths.  Whatever device
+ * arrays hold, no call reads or writes outside the buffers described here: a page outside [0, n_pages) holds no keys and is
+ * not written, a slot outside the cache is not written.  What is refused per request is said per call.
+ *
+ * Envelope: bf16, head_dim 64 or 128, page_size a power of two from 16 to 4096, n_pages * page_size and max_pages * page_size
+ * below 2^31, stride_token at most 2^24, at most 2^20 requests and 2^28 tokens in a call, no tokens or no requests allowed.
+ * These calls are not bracketed by sp_profile_enable.
+ */
+typedef struct {
+  int32_t n_pages, page_size, n_kv_heads, head_dim;
+  int64_t stride_page, stride_token, stride_head; /* elements, shared by K and V; any order of page / token / head */
+} sp_cache_shape;
+
+/* What sp_cache_plan says of a request. */
+enum { SP_PLAN_OK = 0,
+       SP_PLAN_BAD_LENGTH = 1, /* a negative number, more pages held than a row has, or a context longer than the pages held */
+       SP_PLAN_TOO_LONG = 2,   /* ctx_len + new_len exceeds max_pages * page_size, or new_len exceeds 64 * mask_words (if any) */
+       SP_PLAN_NO_ROOM = 3,    /* its tokens end behind max_tokens */
+       SP_PLAN_NO_PAGES = 4 }; /* not enough free pages */
+
+sp_status sp_cache_plan_workspace_bytes(int32_t n_requests, size_t *bytes);
+
+/*
+ * Pages, slots, positions and ancestors of a step's new tokens.
+ *   start      tok_start[r + 1] = min(sum over r' <= r of max(new_len[r'], 0), max_tokens), tok_start[0] = 0
+ *   status     the first reason above that applies to request r, in that order
+ *   pages      request r lacks ceil((ctx_len + new_len) / page_size) - n_held pages (0 if negative or refused for reasons 1 to
+ *              3).  Requests are served in order from the end of the list of free pages: the j-th page of all requests is
+ *              free_pages[n_free - 1 - j]; a request for which they do not suffice gets none, and so does every later one
+ *              that lacks any.  Fresh pages are appended to the request's row; other entries of block_table stay as they are.
+ *   slots      of new token i of a request that is served: that of its position ctx_len + i; -1 for the tokens of refused
+ *              requests and for rows behind the last token, so that a padded batch writes nothing
+ *   positions  ctx_len + depth of the token in its tree (without parents: ctx_len + i); 0 where the slot is -1
+ *   tree_mask  bit j % 64 of word j / 64: new token j is an ancestor of the token, or the token itself (without parents:
+ *              all tokens up to it); 0 where the slot is -1
+ *   seq_len    ctx_len + new_len, or 0 for a refused request
+ *   n_free     at most free_capacity and at least 0 of it counts; n_free_out is what is left of it
+ *
+ *   ctx_len, new_len, n_held   device int32 [n_requests]
+ *   block_table                device int32 [n_requests][max_pages]    (input and output)
+ *   free_pages                 device int32 [free_capacity]; n_free: device int32 [1]
+ *   parents                    device int32 [max_tokens], packed: the parent of a new token, counted from its request's first;
+ *                              -1 (and whatever is not an earlier token): none.  NULL: every request's tokens are a chain
+ *   n_held_out, n_free_out     device int32 [n_requests], [1]; may be n_held's and n_free's own memory
+ *   tok_start, seq_len, status device int32 [n_requests + 1], [n_requests], [n_requests]  (outputs; distinct memory)
+ *   positions, slots           device int32 [max_tokens]               (outputs)
+ *   tree_mask                  device uint64 [max_tokens][mask_words], mask_words 1 to 4; NULL and 0: none  (output)
+ *   workspace                  sp_cache_plan_workspace_bytes(n_requests)
+ */
+sp_status sp_cache_plan(int32_t n_requests, int32_t max_tokens, int32_t page_size, int32_t max_pages, const int32_t *ctx_len,
+                        const int32_t *new_len, const int32_t *n_held, int32_t *block_table, const int32_t *free_pages,
+                        int32_t free_capacity, const int32_t *n_free, const int32_t *parents, int32_t mask_words,
+                        int32_t *n_held_out, int32_t *n_free_out, int32_t *tok_start, int32_t *seq_len, int32_t *positions,
+                        int32_t *slots, int32_t *status, uint64_t *tree_mask, void *workspace, size_t workspace_bytes,
+                        void *hip_stream);
+
+/* Geometry of sp_qk_norm_rope: rows of n_tokens tokens; strides in elements, head_dim contiguous. */
+typedef struct {
+  int32_t n_tokens, n_q_heads, n_kv_heads, head_dim;
+  int32_t rotary_dim;  /* leading elements of a head that are rotated: a multiple of 8, 0 = none */
+  int32_t interleaved; /* pairs (2i, 2i + 1) instead of (i, i + rotary_dim / 2) */
+  int64_t q_stride_t, q_stride_h, k_stride_t, k_stride_h, v_stride_t, v_stride_h;
+  int64_t qo_stride_t, qo_stride_h, ko_stride_t, ko_stride_h;
+  float eps;
+} sp_rope_shape;
+
+/*
+ * Norm of every query and key head, rotation by position, and the cache's write, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * weight over head_dim (weight NULL: y = x), then for pair p of the rotated part
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t), t = position * inv_freq[p], formed in 64 bits.
+ * Rounded to bf16 once.  Queries go to q_out; keys to k_out and, with a cache, to their slots, where values go as they are.
+ * q_out and k_out are what sp_prefill_layer and the other prefill calls take as q and k.
+ *   q, k, v             device bf16 (v only with a cache)
+ *   q_weight, k_weight  device bf16 [head_dim] or NULL (no norm)
+ *   inv_freq            device fp32 [rotary_dim / 2]; positions: device int32 [n_tokens] (not read with rotary_dim 0)
+ *   q_out               device bf16; may be q's memory with q's strides
+ *   k_out               device bf16 or NULL (only the cache); may be k's memory with k's strides
+ *   cache               NULL (no cache), or its geometry with k_cache, v_cache and slots (device int32 [n_tokens]); two tokens
+ *                       with one slot: which of them stays is not said
+ */
+sp_status sp_qk_norm_rope(const sp_rope_shape *shape, const void *q, const void *k, const void *v, const void *q_weight,
+                          const void *k_weight, const float *inv_freq, const int32_t *positions, void *q_out, void *k_out,
+                          const sp_cache_shape *cache, void *k_cache, void *v_cache, const int32_t *slots, void *hip_stream);
+
+/* Geometry of a step's attention; strides in elements, head_dim contiguous. */
+typedef struct {
+  int32_t n_requests;
+  int32_t n_tokens;   /* rows of q and o: at least tok_start[n_requests] */
+  int32_t n_q_heads;
+  int32_t max_new;    /* new tokens of a request that the tiles are laid out for (more are right too, with mask_words 0) */
+  int32_t max_pages;  /* row length of the block table */
+  int32_t mask_words; /* 0: every request's new tokens are a chain */
+  int64_t q_stride_t, q_stride_h, o_stride_t, o_stride_h;
+  float softmax_scale; /* 0 => 1/sqrt(head_dim) */
+} sp_step_shape;
+
+sp_status sp_cache_attn_workspace_bytes(const sp_step_shape *shape, const sp_cache_shape *cache, size_t *bytes);
+
+/*
+ * Attention of the requests' new tokens over the cache.  New token i of request r sees the seq_len[r] - (its new tokens) tokens
+ * of the context and those new tokens j whose bit is set in its tree_mask words (mask_words 0: j <= i); bits of tokens that
+ * do not exist mean nothing.  Query head h reads KV head h / (n_q_heads / n_kv_heads).
+ *   o = sum_s p_s v_s, p = softmax of scale * q.k over the keys that are seen;  lse = ln sum_s e^(scale * q.k_s)
+ * A row that sees no key (a refused request, pages that do not exist, an empty mask) gets o = 0 and lse = -inf.  Keys and values
+ * that a row does not see do not touch it, whatever they hold (NaN and infinities among them).  Rows of o and lse behind
+ * tok_start[n_requests] are left as they were.  A request with seq_len below its number of new tokens counts as refused.
+ * tok_start that falls anywhere: nothing is written.
+ *   q           device bf16 [n_tokens][n_q_heads][head_dim] (strides as given)
+ *   k_cache, v_cache, block_table, seq_len, tok_start, tree_mask  as sp_cache_plan and sp_qk_norm_rope leave them
+ *   o           device bf16 (output);  lse: device fp32 [n_tokens][n_q_heads] or NULL (output)
+ *   workspace   sp_cache_attn_workspace_bytes(shape, cache)
+ */
+sp_status sp_cache_attn(const sp_step_shape *shape, const sp_cache_shape *cache, const void *q, const void *k_cache,
+                        const void *v_cache, const int32_t *block_table, const int32_t *seq_len, const int32_t *tok_start,
+                        const uint64_t *tree_mask, void *o, float *lse, void *workspace, size_t workspace_bytes,
+                        void *hip_stream);
+
+/*
+ * Accepted drafted tokens close up behind the context: for every request and layer, position ctx_len + i takes the rows of
+ * position ctx_len + path[i], i = 0, 1, .., n_accepted - 1, in this order; the rows of a path were rotated by their depth, which
+ * is where they come to lie.  The path ends before the first entry that does not exceed its predecessor, is negative, or is
+ * not below seq_len - ctx_len.  ctx_out = ctx_len + entries of the path.  A move from or to a page that does not exist is left out.
+ *   k_cache, v_cache       device bf16, n_layers caches of the given geometry, stride_layer elements apart
+ *   ctx_len, seq_len, n_accepted  device int32 [n_requests];  path: device int32 [n_requests][max_accept], max_accept <= 256
+ *   ctx_out                device int32 [n_requests] or NULL; not ctx_len's or seq_len's memory
+ */
+sp_status sp_cache_accept(const sp_cache_shape *cache, int32_t n_layers, int64_t stride_layer, void *k_cache, void *v_cache,
+                          int32_t n_requests, int32_t max_pages, const int32_t *block_table, const int32_t *ctx_len,
+                          const int32_t *seq_len, int32_t max_accept, const int32_t *path, const int32_t *n_accepted,
+                          int32_t *ctx_out, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

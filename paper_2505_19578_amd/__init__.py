@@ -18,6 +18,10 @@ from .binding import (SpError, SpShape, lib, shape_of, sp_workspace_bytes, sp_pr
                       SP_FALLBACK_VERTICAL_SLASH_TOKEN, sp_vs_token_workspace_bytes, sp_vertical_slash_attn,
                       SP_SCORE_BLOCK_MASS, SP_SCORE_MEAN_LOGIT, SP_SELECT_PER_ROW, SP_SELECT_GLOBAL,
                       )
+from .cache_binding import (SpCacheShape, SpRopeShape, SpStepShape, cache_shape_of, rope_shape_of, step_shape_of,
+                            sp_cache_plan_workspace_bytes, sp_cache_plan, sp_qk_norm_rope,
+                            sp_cache_attn_workspace_bytes, sp_cache_attn, sp_cache_accept, SP_PLAN_OK,
+                            SP_PLAN_BAD_LENGTH, SP_PLAN_TOO_LONG, SP_PLAN_NO_ROOM, SP_PLAN_NO_PAGES)
 
 __all__ = ["SpError", "SpShape", "lib", "shape_of", "sp_workspace_bytes", "sp_profile_enable", "sp_profile_read",
            "sp_dense_attn_with_block_scores", "sp_build_block_mask",
@@ -30,4 +34,8 @@ __all__ = ["SpError", "SpShape", "lib", "shape_of", "sp_workspace_bytes", "sp_pr
            "sp_vs_workspace_bytes", "sp_search_vertical_slash", "SP_FALLBACK_DENSE", "SP_FALLBACK_VERTICAL_SLASH",
            "SP_FALLBACK_VERTICAL_SLASH_TOKEN", "sp_vs_token_workspace_bytes", "sp_vertical_slash_attn",
            "SP_SCORE_BLOCK_MASS", "SP_SCORE_MEAN_LOGIT", "SP_SELECT_PER_ROW", "SP_SELECT_GLOBAL",
+           "SpCacheShape", "SpRopeShape", "SpStepShape", "cache_shape_of", "rope_shape_of", "step_shape_of",
+           "sp_cache_plan_workspace_bytes", "sp_cache_plan", "sp_qk_norm_rope", "sp_cache_attn_workspace_bytes",
+           "sp_cache_attn", "sp_cache_accept", "SP_PLAN_OK", "SP_PLAN_BAD_LENGTH", "SP_PLAN_TOO_LONG",
+           "SP_PLAN_NO_ROOM", "SP_PLAN_NO_PAGES",
            ]

@@ -19,6 +19,8 @@ EXPORTED_SYMBOLS = [
     "sp_build_block_mask_global", "sp_build_block_mask_global_static", "sp_prefill_layer_modes",
     "sp_determine_pattern", "sp_block_sparse_attn_gated", "sp_prefill_layer_gated", "sp_prefill_layer_dict",
     "sp_vs_workspace_bytes", "sp_search_vertical_slash", "sp_vs_token_workspace_bytes", "sp_vertical_slash_attn",
+    "sp_cache_plan_workspace_bytes", "sp_cache_plan", "sp_qk_norm_rope", "sp_cache_attn_workspace_bytes", "sp_cache_attn",
+    "sp_cache_accept",
 ]
 
 SP_FALLBACK_DENSE, SP_FALLBACK_VERTICAL_SLASH, SP_FALLBACK_VERTICAL_SLASH_TOKEN = 0, 1, 2
@@ -127,6 +129,8 @@ def lib() -> ctypes.CDLL:
         L.sp_vertical_slash_attn.restype = ctypes.c_int
         L.sp_vertical_slash_attn.argtypes = [sp, vp, vp, vp, ip, ctypes.c_int32, ctypes.c_float, ctypes.c_int32, vp, vp,
                                              vp, vp, ctypes.c_size_t, vp]
+        from . import cache_binding
+        cache_binding.declare(L)
         _lib = L
     return _lib
 

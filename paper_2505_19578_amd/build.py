@@ -3,31 +3,47 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = os.path.join(HERE, "csrc", "shareprefill.hip")
+CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libshareprefill.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed fp32 instructions are kept out of the generated code on purpose
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # device code never relies on NaN semantics (the score quantiser tests bits); lets fmax chains
-    # compile to v_max3 without a canonicalising v_max per operand
-    "-Xarch_device", "-fno-honor-nans",
-    "-I" + os.path.join(ROOT, "include"), "-I" + os.path.join(HERE, "csrc"),
+    "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
 ]
+# the translation units and what each is compiled with besides
+SOURCES = {
+    # the prefill's device code never relies on NaN semantics (the score quantiser tests bits); lets fmax chains
+    # compile to v_max3 without a canonicalising v_max per operand
+    "shareprefill.hip": ["-Xarch_device", "-fno-honor-nans"],
+    # the cache's device code does: a value that is not finite stays with the rows that see it
+    "cache.hip": [],
+}
 
 
 def build_library(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + [SRC, "-o", LIB]
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, name + ".o") for name in SOURCES]
+        jobs = []
+        for (name, more), obj in zip(SOURCES.items(), objects):
+            cmd = [hipcc] + HIPCC_FLAGS + more + ["-c", os.path.join(CSRC, name), "-o", obj]
+            jobs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+        out = [job.communicate()[0] for job in jobs]
+        for job, text in zip(jobs, out):
+            if job.returncode != 0:
+                raise RuntimeError("hipcc failed:\n" + text)
+        res = subprocess.run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared"] + objects + ["-o", LIB],
+                             stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if res.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + res.stdout)
     if verbose:
-        print(res.stdout)
+        print("".join(out) + res.stdout)
     return LIB
 
 

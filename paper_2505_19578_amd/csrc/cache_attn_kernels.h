@@ -1,0 +1,771 @@
+// Attention of the requests' new tokens (one, a chain or a drafted tree) over the paged key/value cache.
+#ifndef SP_CACHE_ATTN_KERNELS_H
+#define SP_CACHE_ATTN_KERNELS_H
+#include "cache_common.h"
+
+namespace {
+
+// Per query row (token, head): x = scale q.k over the keys it sees, o = sum 2^(x c - m) v / sum 2^(x c - m), one pass with a running
+// reference m, in fp32.  The query rows of a request that share a KV head (group * tokens) are one matrix: a tile of them meets
+// each key once.
+//
+// Products (v_mfma_f32_16x16x32_bf16; lane = 16 g + i): A (16 x 32) row i, k = 8g .. 8g+7; B (32 x 16) column i, the same k;
+// D (16 x 16) column i, rows 4g .. 4g+3.  S^T = K Q^T puts a query into one column of lanes; its weights, rounded to bf16, are the
+// B operand of O^T = V^T P^T if k slot (g, e) stands for key 4g + e (e < 4) and 16 + 4g + e - 4 (e >= 4) of the step's 32 keys.
+// V comes from LDS transposed (ds_read_b64_tr_b16: 16 lanes read four rows of 16 elements, lane i gets column i).
+//
+// Two kernels.  cache_attn_narrow_kernel (few rows: decoding, small trees; bound by HBM): every wavefront takes steps of 32 keys by
+// itself.  cache_attn_wide_kernel (many rows; bound by the matrix pipe and the softmax): the four wavefronts share K and V in LDS and
+// split the rows.
+//
+// Long contexts are cut into chunks (cache_chunk_units), which cache_join_kernel joins in their order: no atomics, and the bits of
+// a request do not depend on what else the call holds.
+constexpr int CA_THREADS = 256, CA_WAVES = 4;
+constexpr float CA_SLACK = 8.0f;  // how far (log2) a row's maximum may outgrow its reference before the reference moves
+
+struct CacheAttnParams {
+  const uint16_t *q, *k, *v;
+  uint16_t *o;
+  float *lse;
+  const int32_t *table, *seq, *start;
+  const uint64_t *mask;
+  float *part_o, *part_ml;  // [partial rows][D], [partial rows][4]: reference, sum, sum of rounded weights
+  int64_t q_st, q_sh, o_st, o_sh, c_sp, c_st, c_sh;
+  int64_t most_keys;
+  int n_req, n_tok, hq, hk, group, page_shift, n_pages, width, words;
+  float c;  // softmax scale * log2(e)
+};
+
+__device__ __forceinline__ int wave_prefix(int x, int lane) {  // inclusive
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// A request as the workgroups of a call see it.
+struct CacheRequest {
+  CacheShare s;
+  int r;
+  int items_before;  // workgroups' items of the requests before it
+  int rows_before;   // rows of partial results of the requests before it
+};
+
+// Walks the requests of a call forward, 64 at a time, one to a lane.
+template <int TILE>
+struct CacheWalk {
+  const CacheAttnParams &p;
+  const int lane;
+  int r0 = 0, items = 0, rows = 0;  // requests, items and rows of partial results before the present 64
+  int first, end, keys;  // of this lane's request, as the arrays hold them
+  int upto, parts;       // items and rows up to and with it
+  bool good;
+  __device__ __forceinline__ CacheWalk(const CacheAttnParams &params, int l) : p(params), lane(l) { look(); }
+  __device__ __forceinline__ void look() {
+    const int r = r0 + lane;
+    const bool live = r < p.n_req;
+    first = live ? p.start[r] : 0, end = live ? p.start[r + 1] : 0, keys = live ? p.seq[r] : 0;
+    const CacheShare s = cache_share(first, end, keys, p.n_tok, p.most_keys, p.group, TILE);
+    good = !any_lane(end < first);  // otherwise this is no tok_start: nothing behind is done, so that no index leaves its buffer
+    upto = items + wave_prefix(s.tiles * p.hk * s.chunks, lane);
+    parts = rows + wave_prefix(s.chunks > 1 ? s.rows * p.hk * s.chunks : 0, lane);
+  }
+  template <class Test>
+  __device__ __forceinline__ bool seek(Test &&test, CacheRequest &out) {
+    for (;;) {
+      if (!good) return false;
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(test(*this));
+      if (hit) {
+        const int at = __builtin_ctzll(hit);
+        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
+        out.s = cache_share(of(first), of(end), of(keys), p.n_tok, p.most_keys, p.group, TILE);
+        out.r = r0 + at;
+        out.items_before = of(upto) - out.s.tiles * p.hk * out.s.chunks;
+        out.rows_before = of(parts) - (out.s.chunks > 1 ? out.s.rows * p.hk * out.s.chunks : 0);
+        return true;
+      }
+      if (r0 + 64 >= p.n_req) return false;
+      items = __builtin_amdgcn_readlane(upto, 63);
+      rows = __builtin_amdgcn_readlane(parts, 63);
+      r0 += 64;
+      look();
+    }
+  }
+  __device__ __forceinline__ bool item(int index, CacheRequest &out) {
+    return seek([index](const CacheWalk &w) { return w.upto > index; }, out);
+  }
+  __device__ __forceinline__ bool token(int t, CacheRequest &out) {
+    return seek([t](const CacheWalk &w) { return w.end > w.first && w.end > t; }, out);
+  }
+};
+
+// One workgroup's item: a tile of a request's rows under one KV head, and a chunk of its keys.
+struct CacheItem {
+  int kvh, tile, chunk;
+  int k_begin, k_end;  // keys
+  int ctx;             // the request's new tokens begin here (negative without keys: nothing is walked then)
+};
+__device__ __forceinline__ CacheItem item_of(const CacheRequest &rq, int index, int hk) {
+  const CachePlace place = cache_place(index - rq.items_before, rq.s.chunks * hk, rq.s.tiles);
+  CacheItem it;
+  it.chunk = place.pair / hk;
+  it.kvh = place.pair - it.chunk * hk;
+  it.tile = place.tile;
+  const int per = (rq.s.units + rq.s.chunks - 1) / rq.s.chunks;
+  it.k_begin = it.chunk * per * CACHE_UNIT;
+  it.k_end = min(rq.s.keys, it.k_begin + per * CACHE_UNIT);
+  it.ctx = rq.s.keys - rq.s.fresh;
+  return it;
+}
+// where a row's partial result of a chunk lies: a row's chunks side by side
+__device__ __forceinline__ int64_t partial_row(const CacheRequest &rq, int kvh, int row, int chunk) {
+  return rq.rows_before + ((int64_t)kvh * rq.s.rows + row) * rq.s.chunks + chunk;
+}
+
+__device__ __forceinline__ bool odd_bf16x2(uint32_t x) {  // an infinity or NaN in either half
+  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+}
+__device__ __forceinline__ uint32_t without_odd(uint32_t x) {
+  return ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
+}
+// 1.0 where the half is of this kind: infinity, -infinity, NaN
+constexpr int ODD_KINDS = 3;
+__device__ __forceinline__ uint32_t ones_of_kind(uint32_t x, int kind) {
+  uint32_t y = 0;
+#pragma unroll
+  for (int half = 0; half < 32; half += 16) {
+    const uint32_t z = (x >> half) & 0xffffu;
+    const bool hit = kind == 0 ? z == 0x7f80u : kind == 1 ? z == 0xff80u : (z & 0x7fffu) > 0x7f80u;
+    y |= hit ? 0x3f80u << half : 0u;
+  }
+  return y;
+}
+__device__ __forceinline__ float value_of_kind(int kind) {
+  return kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __builtin_nanf("");
+}
+
+typedef __attribute__((address_space(3))) bf16x4 *lds_bf16x4;
+__device__ __forceinline__ bf16x8 read_transposed(char *low, char *high) {
+  const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)low);
+  const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)high);
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// The rows of a wavefront: NC column groups of 16 queries, and what a step of 32 keys does to them.
+template <int D, int NC>
+struct CacheRows {
+  static constexpr int KS = D / 32, DT = D / 16;  // k-steps of S^T, row tiles of O^T
+  bf16x8 q[NC][KS];
+  f32x4 o[NC][DT], ones[NC];
+  float m[NC], l[NC];
+
+  __device__ __forceinline__ void begin(const CacheAttnParams &p, const CacheRequest &rq, int kvh, int row0, int g, int i) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int row = row0 + 16 * c + i;
+      const bool live = row < rq.s.rows;
+      const int t = live ? row / p.group : 0, hq = kvh * p.group + (live ? row - t * p.group : 0);
+      const uint16_t *src = p.q + (int64_t)(rq.s.first + t) * p.q_st + (int64_t)hq * p.q_sh + 8 * g;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        u32x4 x = *(const u32x4 *)(src + 32 * s);
+        if (!live) x = u32x4{0, 0, 0, 0};
+        q[c][s] = __builtin_bit_cast(bf16x8, x);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[c][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+      ones[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m[c] = -INFINITY;
+      l[c] = 0.f;
+    }
+  }
+  // bits of the step's keys that a row sees, from key 4 g of each half on (bits 0 .. 3 and 16 .. 19)
+  static __device__ __forceinline__ uint32_t sees(const CacheAttnParams &p, const CacheRequest &rq, const CacheItem &it, int row,
+                                                  int kb, uint32_t there, int g) {
+    const int t = row < rq.s.rows ? row / p.group : 0;
+    const uint64_t *mask = p.words ? p.mask + (int64_t)(rq.s.first + t) * p.words : nullptr;
+    return (cache_visible(kb, it.ctx, rq.s.fresh, t, mask, p.words) & there) >> (4 * g);
+  }
+  // Weights of a step whose products are x (keys that are not seen: -infinity), as the B operand of the next product.
+  __device__ __forceinline__ void weigh(const f32x4 (&x)[2][NC], float scale, bf16x8 (&pf)[NC]) {
+    float top[NC];
+    bool grow = false;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float t = fmaxf(fmaxf(x[0][c][0], x[0][c][1]), fmaxf(x[0][c][2], x[0][c][3]));
+      t = fmaxf(t, fmaxf(fmaxf(x[1][c][0], x[1][c][1]), fmaxf(x[1][c][2], x[1][c][3])));
+      top[c] = t * scale;
+      grow |= top[c] > m[c] + CA_SLACK;
+    }
+    if (any_lane(grow)) {  // rare: the reference only has to stay within 2^SLACK of the maximum
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float t = top[c];
+        t = fmaxf(t, __shfl_xor(t, 16));
+        t = fmaxf(t, __shfl_xor(t, 32));
+        const float to = t > m[c] + CA_SLACK ? t : m[c];
+        const float f = to == m[c] ? 1.f : __builtin_amdgcn_exp2f(m[c] - to);
+        m[c] = to;
+        l[c] *= f;
+        ones[c] *= f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[c][d] *= f;
+      }
+    }
+    const uint32_t one2 = 0x3f803f80u;
+    const bf16x8 all_ones = __builtin_bit_cast(bf16x8, (u32x4{one2, one2, one2, one2}));
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float e[8];
+      const float ref = m[c] == -INFINITY ? 0.f : m[c];  // (nothing seen yet: weights are 2^-infinity)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          e[4 * j + r] = __builtin_amdgcn_exp2f(x[j][c][r] * scale - ref);
+          l[c] += e[4 * j + r];
+        }
+      // The weights are rounded to bf16 for the product (relative 2^-8 at most each).  O is divided by the sum of the rounded
+      // ones, which the matrix pipe forms with a row of ones, so a row that few keys dominate keeps no error of its sum;
+      // lse is that of the unrounded sum.
+      const u32x4 y = {pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7])};
+      pf[c] = __builtin_bit_cast(bf16x8, y);
+      ones[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all_ones, pf[c], ones[c], 0, 0, 0);
+    }
+  }
+  // O += V P, V's fragments as read(d) gives them
+  template <class Read>
+  __device__ __forceinline__ void add_values(const bf16x8 (&pf)[NC], Read &&read) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      const bf16x8 a = read(d);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf[c], o[c][d], 0, 0, 0);
+    }
+  }
+  // what `see` of a step's columns says, as a B operand of ones and zeros
+  static __device__ __forceinline__ bf16x8 as_ones(uint32_t see) {
+    u32x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int bit = 16 * (e >> 1) + 2 * (e & 1);
+      y[e] = ((see >> bit) & 1 ? 0x3f80u : 0u) | ((see >> (bit + 1)) & 1 ? 0x3f800000u : 0u);
+    }
+    return __builtin_bit_cast(bf16x8, y);
+  }
+  // O += the kind's value where a row sees a value of this kind: V's fragments are 1 where a value is of the kind
+  template <class Read>
+  __device__ __forceinline__ void add_kind(const bf16x8 (&seen)[NC], int kind, Read &&read) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      const bf16x8 a = read(d);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, seen[c], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (n[r] > 0.f) o[c][d][r] += value_of_kind(kind);
+      }
+    }
+  }
+  // row sums over the lanes that share a column
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      l[c] += __shfl_xor(l[c], 16);
+      l[c] += __shfl_xor(l[c], 32);
+    }
+  }
+};
+
+__device__ __forceinline__ float lse_of(float ref, float sum) {
+  return sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+
+// ---------------------------------------------------------------------------------------------------------------- narrow
+// A wavefront has its own registers and its own piece of LDS (V on its way to the transposed read), and no barrier until the
+// workgroup's four wavefronts add up at the end.  K goes from memory to the A registers as it lies.  K of the next step is asked
+// for as soon as the products have read this one's, V as soon as it lies in LDS; two workgroups on a compute unit keep 128 KiB in flight.
+template <int D, int NC>
+__global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_narrow_kernel(CacheAttnParams p) {
+  constexpr int ROWS = 16 * NC;        // query rows of the tile
+  constexpr int KS = D / 32, DT = D / 16;
+  constexpr int NV = D / 16;           // 16-byte loads of a lane for a step's V
+  constexpr int VL = D / 8;            // lanes of a V row
+  constexpr int VROW = 2 * D + 32;     // bytes of a V row in LDS: 16 lanes' reads of four rows, and writes, meet no bank twice
+  constexpr int OROW = D + 4;          // floats of an O row in LDS
+  constexpr int V_BYTES = CACHE_STEP * VROW, SUM_BYTES = CA_WAVES * 16 * OROW * 4;
+  constexpr int LDS = CA_WAVES * V_BYTES > SUM_BYTES ? CA_WAVES * V_BYTES : SUM_BYTES;
+  __shared__ __attribute__((aligned(16))) char smem[LDS];
+  __shared__ float sm[CA_WAVES][ROWS], sl[CA_WAVES][ROWS], sr[CA_WAVES][ROWS];
+
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, i = lane & 15;
+  const int w = uniform(tid >> 6);
+  char *const v_lds = smem + w * V_BYTES;
+  auto v_fragment = [&](int d) -> bf16x8 {
+    char *at = v_lds + (4 * g + (i >> 2)) * VROW + d * 32 + (i & 3) * 8;
+    return read_transposed(at, at + 16 * VROW);
+  };
+  auto store_v = [&](const u32x4 *x) {
+#pragma unroll
+    for (int n = 0; n < NV; ++n) *(u32x4 *)(v_lds + ((64 / VL) * n + lane / VL) * VROW + (lane % VL) * 16) = x[n];
+  };
+  const uint32_t k_lane = 2u * (uint32_t)(i * (int)p.c_st + 8 * g);  // bytes
+  const uint32_t v_lane = 2u * (uint32_t)((lane / VL) * (int)p.c_st + 8 * (lane % VL));
+
+  CacheWalk<ROWS> walk(p, lane);
+  CacheRequest rq;
+  for (int index = blockIdx.x; walk.item(index, rq); index += gridDim.x) {
+    const CacheItem it = item_of(rq, index, p.hk);
+    CacheRows<D, NC> rows;
+    const int row0 = it.tile * ROWS;
+    rows.begin(p, rq, it.kvh, row0, g, i);
+
+    // Pages of 32 of the wavefront's steps at a time: lane 2 s + half holds that of step s, keys 16 half .. 16 half + 15 (a page
+    // holds 16 keys and more, and begins at a multiple of them); -1: no such key, or a page that the cache does not have.
+    const int32_t *row_pages = p.table + (int64_t)rq.r * p.width;
+    const int first = it.k_begin + CACHE_STEP * w;
+    const int steps = first < it.k_end ? (it.k_end - first + CACHE_UNIT - 1) / CACHE_UNIT : 0;
+    auto step_key = [&](int s) { return first + CACHE_UNIT * s; };
+    int pages = -1, pages_from = 0;
+    auto load_pages = [&](int s0) {
+      const int s = s0 + (lane >> 1), key = step_key(s) + 16 * (lane & 1);
+      pages = -1;
+      if (s < steps && key < it.k_end) {
+        const int id = row_pages[key >> p.page_shift];
+        pages = id >= 0 && id < p.n_pages ? id : -1;
+      }
+      pages_from = s0;
+    };
+    const int64_t head_off = (int64_t)it.kvh * p.c_sh;
+    auto group_base = [&](int id, int key) -> int64_t {
+      return (int64_t)(id < 0 ? 0 : id) * p.c_sp + (int64_t)(key & ((1 << p.page_shift) - 1)) * p.c_st + head_off;
+    };
+    u32x4 kr[2][KS], vr[NV];
+    auto load_k = [&](int key, int id0, int id1) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint16_t *base = p.k + group_base(j ? id1 : id0, key + 16 * j);
+#pragma unroll
+        for (int x = 0; x < KS; ++x) kr[j][x] = *(const u32x4 *)((const char *)base + k_lane + 64 * x);
+      }
+    };
+    auto load_v = [&](int key, int id0, int id1) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint16_t *base = p.v + group_base(j ? id1 : id0, key + 16 * j);
+#pragma unroll
+        for (int x = 0; x < NV / 2; ++x)
+          vr[j * (NV / 2) + x] = *(const u32x4 *)((const char *)(base + (int64_t)(64 / VL) * x * p.c_st) + v_lane);
+      }
+    };
+    int id0 = -1, id1 = -1;  // pages of the step whose keys are being loaded
+    auto take_ids = [&](int s) {
+      if (s - pages_from >= 32) load_pages(s);
+      id0 = __builtin_amdgcn_readlane(pages, 2 * (s - pages_from));
+      id1 = __builtin_amdgcn_readlane(pages, 2 * (s - pages_from) + 1);
+    };
+
+    if (steps > 0) {
+      load_pages(0);
+      take_ids(0);
+      load_k(step_key(0), id0, id1);
+      load_v(step_key(0), id0, id1);
+    }
+    for (int s = 0; s < steps; ++s) {
+      const int kb = step_key(s), was0 = id0, was1 = id1;
+      f32x4 x[2][NC];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int y = 0; y < KS; ++y)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[j][y]), rows.q[c][y], acc, 0, 0, 0);
+          x[j][c] = acc;
+        }
+      if (s + 1 < steps) {
+        take_ids(s + 1);
+        load_k(step_key(s + 1), id0, id1);
+      }
+      // all keys of a step in the context are seen by every row
+      const bool whole = kb + CACHE_STEP <= it.ctx && was0 >= 0 && was1 >= 0;
+      const uint32_t there = (was0 < 0 ? 0u : 0xffffu) | (was1 < 0 ? 0u : 0xffff0000u);
+      auto no_value = [&](int n) { return kb + (64 / VL) * n + lane / VL >= it.k_end || (n < NV / 2 ? was0 : was1) < 0; };
+      bool odd_values = false;
+      if (!whole) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const uint32_t see = rows.sees(p, rq, it, row0 + 16 * c + i, kb, there, g);
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (!((see >> (16 * j + r)) & 1)) x[j][c][r] = -INFINITY;
+        }
+        // values of keys that do not exist count as zeros; values that are not finite are kept out of the product and added to
+        // the rows that see them (below)
+        bool odd = false;
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          if (no_value(n)) vr[n] = u32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            odd |= odd_bf16x2(vr[n][e]);
+            vr[n][e] = without_odd(vr[n][e]);
+          }
+        }
+        odd_values = any_lane(odd);
+      }
+      store_v(vr);
+      bf16x8 pf[NC];
+      rows.weigh(x, p.c, pf);
+      if (!odd_values && s + 1 < steps) load_v(step_key(s + 1), id0, id1);
+      rows.add_values(pf, v_fragment);
+      if (odd_values) {
+        bf16x8 seen[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) seen[c] = rows.as_ones(rows.sees(p, rq, it, row0 + 16 * c + i, kb, there, g));
+#pragma unroll 1
+        for (int kind = 0; kind < ODD_KINDS; ++kind) {
+          load_v(kb, was0, was1);
+#pragma unroll
+          for (int n = 0; n < NV; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vr[n][e] = no_value(n) ? 0u : ones_of_kind(vr[n][e], kind);
+          store_v(vr);
+          rows.add_kind(seen, kind, v_fragment);
+        }
+        if (s + 1 < steps) load_v(step_key(s + 1), id0, id1);
+      }
+    }
+
+    // the four wavefronts add up, sixteen rows at a time
+    rows.finish();
+    __syncthreads();  // (the last item's sums are read)
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (g == 0) {
+        sm[w][16 * c + i] = rows.m[c];
+        sl[w][16 * c + i] = rows.l[c];
+        sr[w][16 * c + i] = rows.ones[c][0];
+      }
+    const int orow = tid >> 4, piece = tid & 15;  // this thread's row and its D / 16 elements of it
+    float *const sum = (float *)smem;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      __syncthreads();
+      {
+        float top = sm[0][16 * c + i];
+#pragma unroll
+        for (int x = 1; x < CA_WAVES; ++x) top = fmaxf(top, sm[x][16 * c + i]);
+        const float f = rows.m[c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rows.m[c] - top);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          *(f32x4 *)(sum + (w * 16 + i) * OROW + 16 * d + 4 * g) = f == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : rows.o[c][d] * f;
+      }
+      __syncthreads();
+      const int row = it.tile * ROWS + 16 * c + orow;
+      float top = -INFINITY, ls = 0.f, lr = 0.f;
+#pragma unroll
+      for (int x = 0; x < CA_WAVES; ++x) top = fmaxf(top, sm[x][16 * c + orow]);
+#pragma unroll
+      for (int x = 0; x < CA_WAVES; ++x) {
+        const float f = sm[x][16 * c + orow] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[x][16 * c + orow] - top);
+        ls += f * sl[x][16 * c + orow];
+        lr += f * sr[x][16 * c + orow];
+      }
+      constexpr int E = D / 16;
+      float y[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = 0.f;
+#pragma unroll
+      for (int x = 0; x < CA_WAVES; ++x)
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+          const f32x4 z = *(const f32x4 *)(sum + (x * 16 + orow) * OROW + E * piece + e);
+          y[e] += z[0], y[e + 1] += z[1], y[e + 2] += z[2], y[e + 3] += z[3];
+        }
+      if (row >= rq.s.rows) continue;
+      if (rq.s.chunks > 1) {
+        const int64_t at = partial_row(rq, it.kvh, row, it.chunk);
+#pragma unroll
+        for (int e = 0; e < E; e += 4) *(f32x4 *)(p.part_o + at * D + E * piece + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
+        if (piece == 0) *(f32x4 *)(p.part_ml + at * 4) = f32x4{top, ls, lr, 0.f};
+      } else {
+        const int t = row / p.group, hq = it.kvh * p.group + row - t * p.group;
+        const float inv = inverse(lr);
+        uint16_t *dst = p.o + (int64_t)(rq.s.first + t) * p.o_st + (int64_t)hq * p.o_sh + E * piece;
+#pragma unroll
+        for (int e = 0; e < E; e += 4)
+          *(u32x2 *)(dst + e) = u32x2{pack_bf16(y[e] * inv, y[e + 1] * inv), pack_bf16(y[e + 2] * inv, y[e + 3] * inv)};
+        if (p.lse && piece == 0) p.lse[(int64_t)(rq.s.first + t) * p.hq + hq] = lse_of(top, ls);
+      }
+    }
+    __syncthreads();  // the sums lie where V of the next item will
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------ wide
+// One wavefront-wide 1 KiB copy from memory to LDS: lane l moves 16 bytes at g_uniform + lane_off to LDS byte address
+// lds_base + 16 l.  From inline assembly, so that the compiler does not wait for it at the next LDS read: the kernel counts these
+// loads itself (wait_copies), and the compiler's own waits, which count in order, only become stricter by them.
+__device__ __forceinline__ void copy_to_lds(const void *g_uniform, uint32_t lane_off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(lane_off), "s"(g_uniform)
+               : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Steps of 32 keys of K and V lie in a ring in LDS, filled RING - 1 steps ahead by copies that pass no registers; one barrier a
+// step.  A row's 16-byte pieces lie XOR-swizzled by the row number, so that the fragments' reads (16 rows at a time for K, four
+// rows for V) meet no bank twice; the copies' lanes fetch the pieces in that order.
+template <int D, int NC>
+__global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAttnParams p) {
+  constexpr int WROWS = 16 * NC, ROWS = CA_WAVES * WROWS;
+  constexpr int KS = D / 32, DT = D / 16;
+  constexpr int RING = 4;
+  constexpr int ROWB = 2 * D;                   // bytes of a K or V row
+  constexpr int TILE = CACHE_STEP * ROWB;       // of a step's K (or V)
+  constexpr int PIECES = ROWB / 16;             // 16-byte pieces of a row
+  constexpr int COPY_ROWS = 1024 / ROWB;        // rows that one copy moves
+  constexpr int COPIES = CACHE_STEP / CA_WAVES / COPY_ROWS;  // copies of a wavefront for its 8 rows of K (and as many for V)
+  __shared__ __attribute__((aligned(1024))) char smem[RING * 2 * TILE];
+  const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) char *)smem;
+
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, i = lane & 15;
+  const int w = uniform(tid >> 6);
+  // byte of piece x of row r of a tile
+  auto place = [](int r, int x) { return r * ROWB + ((x ^ (D == 128 ? r & 15 : (r >> 1) & 7)) * 16); };
+  // this lane's part of copy n: row and piece (the LDS side is lane after lane)
+  uint32_t copy_off[COPIES];
+#pragma unroll
+  for (int n = 0; n < COPIES; ++n) {
+    const int r = (CACHE_STEP / CA_WAVES) * w + COPY_ROWS * n + lane / PIECES, slot = lane % PIECES;
+    const int x = slot ^ (D == 128 ? r & 15 : (r >> 1) & 7);
+    copy_off[n] = 2u * (uint32_t)((r & 15) * (int)p.c_st + 8 * x);
+  }
+  auto k_fragment = [&](const char *tile, int j, int s) -> bf16x8 {
+    return *(const bf16x8 *)(tile + place(16 * j + i, 4 * s + g));
+  };
+  auto v_fragment = [&](char *tile, int d) -> bf16x8 {
+    const int r = 4 * g + (i >> 2), x = 2 * d + ((i & 3) >> 1), half = (i & 1) * 8;
+    return read_transposed(tile + place(r, x) + half, tile + place(r + 16, x) + half);
+  };
+
+  CacheWalk<ROWS> walk(p, lane);
+  CacheRequest rq;
+  for (int index = blockIdx.x; walk.item(index, rq); index += gridDim.x) {
+    const CacheItem it = item_of(rq, index, p.hk);
+    CacheRows<D, NC> rows;
+    const int row0 = it.tile * ROWS + w * WROWS;
+    rows.begin(p, rq, it.kvh, row0, g, i);
+    const int32_t *row_pages = p.table + (int64_t)rq.r * p.width;
+    const int steps = it.k_begin < it.k_end ? (it.k_end - it.k_begin + CACHE_STEP - 1) / CACHE_STEP : 0;
+    // pages of 64 steps at a time: lane s holds those of both halves of step s; -1: no such key, or a page that does not exist
+    int half0 = -1, half1 = -1, pages_from = 0;
+    auto page_at = [&](int key) {
+      if (key >= it.k_end) return -1;
+      const int id = row_pages[key >> p.page_shift];
+      return id >= 0 && id < p.n_pages ? id : -1;
+    };
+    auto load_pages = [&](int s0) {
+      const int key = it.k_begin + CACHE_STEP * (s0 + lane);
+      half0 = page_at(key);
+      half1 = page_at(key + 16);
+      pages_from = s0;
+    };
+    const int64_t head_off = (int64_t)it.kvh * p.c_sh;
+    uint64_t bad = 0;  // of the steps in the ring, two bits each (step s: bits 2 (s % 32)): a half without a page
+    auto fetch = [&](int s) {
+      if (s - pages_from >= 64) load_pages(s);
+      const int a = __builtin_amdgcn_readlane(half0, s - pages_from), b = __builtin_amdgcn_readlane(half1, s - pages_from);
+      const int at = 2 * (s & 31);
+      bad = (bad & ~(3ull << at)) | ((uint64_t)((a < 0 ? 1 : 0) | (b < 0 ? 2 : 0)) << at);
+      const int half = w >> 1, id = half ? b : a, key = it.k_begin + CACHE_STEP * s + 16 * half;
+      const int64_t from = (int64_t)(id < 0 ? 0 : id) * p.c_sp + (int64_t)(key & ((1 << p.page_shift) - 1)) * p.c_st + head_off;
+      const uint32_t to = lds0 + (uint32_t)((s % RING) * 2 * TILE + (CACHE_STEP / CA_WAVES) * w * ROWB);
+#pragma unroll
+      for (int n = 0; n < COPIES; ++n) copy_to_lds(p.k + from, copy_off[n], to + 1024 * n);
+#pragma unroll
+      for (int n = 0; n < COPIES; ++n) copy_to_lds(p.v + from, copy_off[n], to + TILE + 1024 * n);
+    };
+    if (steps > 0) load_pages(0);
+    for (int s = 0; s < RING - 1 && s < steps; ++s) fetch(s);
+    for (int s = 0; s < steps; ++s) {
+      if (s + RING - 2 < steps)
+        wait_copies<(RING - 2) * 2 * COPIES>();
+      else
+        wait_copies<0>();
+      __syncthreads();
+      const int gone = (int)((bad >> (2 * (s & 31))) & 3);
+      if (s + RING - 1 < steps) fetch(s + RING - 1);
+      char *const kt = smem + (s % RING) * 2 * TILE, *const vt = kt + TILE;
+      const int kb = it.k_begin + CACHE_STEP * s;
+      f32x4 x[2][NC];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) x[j][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int y = 0; y < KS; ++y) {
+          const bf16x8 a = k_fragment(kt, j, y);
+#pragma unroll
+          for (int c = 0; c < NC; ++c) x[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, rows.q[c][y], x[j][c], 0, 0, 0);
+        }
+      }
+      const bool whole = kb + CACHE_STEP <= it.ctx && !gone;
+      const uint32_t there = (gone & 1 ? 0u : 0xffffu) | (gone & 2 ? 0u : 0xffff0000u);
+      bool odd_values = false;
+      // values of keys that do not exist become zeros; values that are not finite are kept out of the product and added to the
+      // rows that see them
+      constexpr int OWN = TILE / 16 / CA_THREADS;  // pieces of V that are this thread's to look at
+      auto no_value = [&](int at) {
+        const int r = at / ROWB;
+        return kb + r >= it.k_end || ((r < 16 ? gone : gone >> 1) & 1);
+      };
+      if (!whole) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const uint32_t see = rows.sees(p, rq, it, row0 + 16 * c + i, kb, there, g);
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (!((see >> (16 * j + r)) & 1)) x[j][c][r] = -INFINITY;
+        }
+        int odd = 0;
+#pragma unroll
+        for (int n = 0; n < OWN; ++n) {
+          const int at = (n * CA_THREADS + tid) * 16;
+          const u32x4 y = *(const u32x4 *)(vt + at);
+          if (no_value(at))
+            *(u32x4 *)(vt + at) = u32x4{0, 0, 0, 0};
+          else
+            odd |= odd_bf16x2(y[0]) || odd_bf16x2(y[1]) || odd_bf16x2(y[2]) || odd_bf16x2(y[3]);
+        }
+        odd_values = __syncthreads_or(odd) != 0;
+      }
+      bf16x8 pf[NC];
+      rows.weigh(x, p.c, pf);
+      if (odd_values) {
+        bf16x8 seen[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) seen[c] = rows.as_ones(rows.sees(p, rq, it, row0 + 16 * c + i, kb, there, g));
+        u32x4 keep[OWN];
+#pragma unroll
+        for (int n = 0; n < OWN; ++n) keep[n] = *(const u32x4 *)(vt + (n * CA_THREADS + tid) * 16);
+#pragma unroll 1
+        for (int kind = 0; kind <= ODD_KINDS; ++kind) {  // the last round leaves the finite values
+#pragma unroll
+          for (int n = 0; n < OWN; ++n) {
+            u32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = kind == ODD_KINDS ? without_odd(keep[n][e]) : ones_of_kind(keep[n][e], kind);
+            *(u32x4 *)(vt + (n * CA_THREADS + tid) * 16) = y;
+          }
+          __syncthreads();
+          if (kind < ODD_KINDS) {
+            rows.add_kind(seen, kind, [&](int d) { return v_fragment(vt, d); });
+            __syncthreads();
+          }
+        }
+      }
+      rows.add_values(pf, [&](int d) { return v_fragment(vt, d); });
+    }
+    rows.finish();
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int row = row0 + 16 * c + i;
+      if (row >= rq.s.rows) continue;
+      const float lr = rows.ones[c][0];
+      if (rq.s.chunks > 1) {
+        const int64_t at = partial_row(rq, it.kvh, row, it.chunk);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *(f32x4 *)(p.part_o + at * D + 16 * d + 4 * g) = rows.o[c][d];
+        if (g == 0) *(f32x4 *)(p.part_ml + at * 4) = f32x4{rows.m[c], rows.l[c], lr, 0.f};
+      } else {
+        const int t = row / p.group, hq = it.kvh * p.group + row - t * p.group;
+        const float inv = inverse(lr);
+        uint16_t *dst = p.o + (int64_t)(rq.s.first + t) * p.o_st + (int64_t)hq * p.o_sh + 4 * g;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const f32x4 y = rows.o[c][d] * inv;
+          *(u32x2 *)(dst + 16 * d) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+        }
+        if (p.lse && g == 0) p.lse[(int64_t)(rq.s.first + t) * p.hq + hq] = lse_of(rows.m[c], rows.l[c]);
+      }
+    }
+    __syncthreads();  // the ring is read: the next item's steps may be fetched
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------ join
+// Joins the chunks of a row, in their order: a wavefront per row.
+template <int D>
+__global__ __launch_bounds__(CA_THREADS) void cache_join_kernel(CacheAttnParams p) {
+  constexpr int E = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * CA_WAVES + uniform(threadIdx.x >> 6);
+  const int token = (int)(at / p.hq), hq = (int)(at - (int64_t)token * p.hq);
+  if (token >= p.n_tok) return;
+  CacheWalk<16> walk(p, lane);  // (nothing here depends on the tiles)
+  CacheRequest rq;
+  if (!walk.token(token, rq) || rq.s.chunks == 1 || token < rq.s.first) return;
+  const int kvh = hq / p.group, row = (token - rq.s.first) * p.group + hq - kvh * p.group;
+  const int64_t from = partial_row(rq, kvh, row, 0);
+  const int chunks = rq.s.chunks;
+  float top = -INFINITY;
+  for (int c = lane; c < chunks; c += 64) top = fmaxf(top, p.part_ml[(from + c) * 4]);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  float ls = 0.f, lr = 0.f, y[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = 0.f;
+  for (int c0 = 0; c0 < chunks; c0 += 64) {
+    const int n = min(64, chunks - c0);
+    f32x4 ml = {-INFINITY, 0.f, 0.f, 0.f};
+    if (lane < n) ml = *(const f32x4 *)(p.part_ml + (from + c0 + lane) * 4);
+    const float f = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
+    ls += f * ml[1];
+    lr += f * ml[2];
+    const float *src = p.part_o + (from + c0) * D + E * lane;
+    constexpr int AHEAD = 8;
+    for (int c = 0; c < n; c += AHEAD) {
+      float z[AHEAD][E];
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a)
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[a][e] = src[(int64_t)min(c + a, n - 1) * D + e];
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {
+        const float fc = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), (c + a) & 63));
+        if (c + a < n && fc != 0.f)
+#pragma unroll
+          for (int e = 0; e < E; ++e) y[e] += fc * z[a][e];
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    ls += __shfl_xor(ls, d);
+    lr += __shfl_xor(lr, d);
+  }
+  const float inv = inverse(lr);
+  uint16_t *dst = p.o + (int64_t)token * p.o_st + (int64_t)hq * p.o_sh + E * lane;
+  if constexpr (E == 2)
+    *(uint32_t *)dst = pack_bf16(y[0] * inv, y[1] * inv);
+  else
+    *dst = (uint16_t)pack_bf16(y[0] * inv, 0.f);
+  if (p.lse && lane == 0) p.lse[(int64_t)token * p.hq + hq] = lse_of(top, ls);
+}
+
+}  // namespace
+
+#endif

@@ -1,0 +1,123 @@
+// Index arithmetic of the paged key/value cache: what a step sees of a page, of a drafted tree and of the split of long contexts.
+// Plain C++ (constexpr functions also run on the device), so that a test can compile it for the CPU.
+#ifndef SP_CACHE_INDEX_H
+#define SP_CACHE_INDEX_H
+#include <cstddef>
+#include <cstdint>
+
+constexpr int CACHE_MAX_WORDS = 4;        // mask words of a drafted token
+constexpr int CACHE_MIN_PAGE = 16, CACHE_MAX_PAGE = 4096;
+constexpr int CACHE_STEP = 32;            // keys of a wavefront's step
+constexpr int CACHE_UNIT = 4 * CACHE_STEP;  // keys that the four wavefronts of a workgroup take at once
+
+// Refusals of sp_cache_plan, in the order in which they are tested.
+enum CachePlanStatus { PLAN_OK = 0, PLAN_BAD_LENGTH = 1, PLAN_TOO_LONG = 2, PLAN_NO_ROOM = 3, PLAN_NO_PAGES = 4 };
+
+// What the lengths of one request alone say.  `width` pages of `page` tokens a row, at most `most` new tokens.
+constexpr int plan_length_status(int64_t ctx, int64_t fresh, int64_t held, int64_t width, int64_t page, int64_t most) {
+  if (fresh < 0 || ctx < 0 || held < 0 || held > width || held * page < ctx) return PLAN_BAD_LENGTH;
+  if (ctx + fresh > width * page || fresh > most) return PLAN_TOO_LONG;
+  return PLAN_OK;
+}
+// Pages a request lacks for `tokens` tokens when it holds `held`.
+constexpr int64_t plan_lacking(int64_t tokens, int64_t held, int64_t page) {
+  const int64_t need = (tokens + page - 1) / page;
+  return need > held ? need - held : 0;
+}
+// The slot of position `offset` of page `page_id`, -1 where there is none that 32 bits hold.
+constexpr int32_t cache_slot(int64_t page_id, int64_t page, int64_t offset) {
+  const int64_t s = page_id * page + offset;
+  return page_id < 0 || s > 0x7fffffff ? -1 : (int32_t)s;
+}
+
+// Keys kb .. kb + 31 that new token i of a request sees, as bits.  The request has `ctx` tokens in the cache before its `fresh`
+// new ones; new token j lies at position ctx + j.  words != 0: bit j of mask[] says whether token i sees new token j; words == 0:
+// it sees tokens 0 .. i.  kb may lie anywhere, also behind the last key.
+constexpr uint32_t cache_visible(int64_t kb, int64_t ctx, int fresh, int i, const uint64_t *mask, int words) {
+  uint64_t seen = 0;  // of new tokens kb - ctx, ..
+  const int64_t j0 = kb - ctx;
+  if (words == 0) {
+    const int64_t last = i < fresh ? i : fresh - 1;  // the last new token that is seen
+    const int64_t n = last - j0 + 1;                 // keys from kb on up to it
+    seen = n <= 0 ? 0 : n >= 32 ? 0xffffffffu : (1ull << n) - 1;
+  } else if (j0 < 64 * (int64_t)words && j0 > -32) {
+    if (j0 >= 0) {
+      const int w = (int)(j0 >> 6), sh = (int)(j0 & 63);
+      seen = mask[w] >> sh;
+      if (sh && w + 1 < words) seen |= mask[w + 1] << (64 - sh);
+    } else {
+      seen = mask[0] << -j0;
+    }
+    const int64_t n = fresh - j0;  // keys from kb on that exist
+    seen &= n <= 0 ? 0 : n >= 32 ? 0xffffffffu : (1ull << n) - 1;
+  }
+  const int64_t before = ctx - kb;  // keys from kb on that lie in the context
+  const uint64_t old = before <= 0 ? 0 : before >= 32 ? 0xffffffffu : (1ull << before) - 1;
+  // a new token's key lies behind the context, whatever bits of the chain's rule fall before it
+  return (uint32_t)((seen & ~old) | old);
+}
+
+// One request's share of an attention call: `rows` query rows per KV head in `tiles` tiles, `units` of CACHE_UNIT keys in
+// `chunks` chunks.
+struct CacheShare {
+  int32_t first, fresh, keys, rows, tiles, units, chunks;
+};
+// Units of a chunk.  It goes by the request's own sizes alone, so that a request's result is the same bits whatever else the
+// call holds: about 16 chunks per 64 rows, so that one request spreads over the chip, of 2 to 16 units per 64 rows, so that a
+// workgroup has enough to do and a long context still makes more workgroups than 16.
+constexpr int64_t cache_chunk_units(int64_t units, int64_t rows) {
+  const int64_t t = (rows + 63) / 64, u = (units * t + 15) / 16;
+  return u < 2 ? 2 : u > 16 * t ? 16 * t : u;
+}
+// Tokens and keys come from device memory: whatever is in it, a share is a share of rows and keys that exist.
+constexpr CacheShare cache_share(int64_t first, int64_t end, int64_t keys, int64_t n_tokens, int64_t most_keys, int group, int tile_rows) {
+  if (first < 0) first = 0;
+  if (end > n_tokens) end = n_tokens;
+  const int64_t fresh = end > first ? end - first : 0;
+  if (keys > most_keys) keys = most_keys;
+  if (keys < fresh) keys = 0;  // a request that the plan refused: no keys, its rows become zeros
+  CacheShare s{};
+  s.first = (int32_t)first, s.fresh = (int32_t)fresh, s.keys = (int32_t)keys;
+  s.rows = (int32_t)(fresh * group);
+  s.tiles = (int32_t)((fresh * group + tile_rows - 1) / tile_rows);
+  s.units = keys > 0 ? (int32_t)((keys + CACHE_UNIT - 1) / CACHE_UNIT) : 1;
+  const int64_t u = cache_chunk_units(s.units, s.rows);
+  s.chunks = (int32_t)((s.units + u - 1) / u);
+  return s;
+}
+// Upper bounds of what all requests of a call add up to, per KV head; the kernels' sums never pass them.
+// chunks <= most / t + 1 with t = ceil(rows / 64) and `most` as follows
+constexpr int64_t cache_most_chunks(int64_t most_keys) {
+  const int64_t units = (most_keys + CACHE_UNIT - 1) / CACHE_UNIT;
+  return units <= 2 ? 1 : units / 16 > 16 ? (units + 15) / 16 : 16;
+}
+// rows of partial results: rows * chunks
+constexpr int64_t cache_partial_rows(int64_t n_requests, int64_t n_tokens, int group, int64_t most_keys) {
+  if (cache_most_chunks(most_keys) == 1) return 0;  // no request has two chunks
+  const int64_t rows = n_tokens * group, wide = rows < 64 * n_requests ? rows : 64 * n_requests;
+  const int64_t live = n_requests < n_tokens ? n_requests : n_tokens;
+  return wide * cache_most_chunks(most_keys) + rows + 63 * live;
+}
+// workgroups: tiles * chunks
+constexpr int64_t cache_grid(int64_t n_requests, int64_t n_tokens, int group, int64_t most_keys, int tile_rows) {
+  const int64_t live = n_requests < n_tokens ? n_requests : n_tokens;
+  const int64_t tiles = n_tokens * group / tile_rows + live, per = tile_rows < 64 ? 64 / tile_rows : 1;
+  const int64_t wide = tiles < per * live ? tiles : per * live;
+  return wide * cache_most_chunks(most_keys) + tiles;
+}
+
+// Place of a workgroup among a request's: `pairs` pairs (chunk, KV head), KV head first, times `tiles`.  Workgroups go round-robin
+// to the 8 XCDs, so pairs are taken eight at a time and the tiles of a pair, which read the same keys, lie eight apart: one L2.
+struct CachePlace {
+  int32_t pair, tile;
+};
+constexpr CachePlace cache_place(int32_t index, int32_t pairs, int32_t tiles) {
+  const int32_t eight = index / (8 * tiles), rest = index - eight * 8 * tiles;
+  const int32_t wide = pairs - 8 * eight < 8 ? pairs - 8 * eight : 8;
+  return CachePlace{8 * eight + rest % wide, rest / wide};
+}
+constexpr int32_t cache_index_of(int32_t pair, int32_t tile, int32_t pairs, int32_t tiles) {
+  const int32_t eight = pair / 8, wide = pairs - 8 * eight < 8 ? pairs - 8 * eight : 8;
+  return eight * 8 * tiles + tile * wide + pair % 8;
+}
+#endif

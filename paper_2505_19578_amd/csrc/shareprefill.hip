@@ -1,7 +1,7 @@
 // SharePrefill prefill attention for one layer on gfx950 (MI355X): HIP kernels + C ABI.
 //
-// This file is the host side (argument checks, workspace layouts, launchers, the C ABI) and the only
-// translation unit; the kernels live in the headers it includes.
+// This file is the host side (argument checks, workspace layouts, launchers, the C ABI); the kernels live in the
+// headers it includes.  The calls around the paged key/value cache are a translation unit of their own (cache.hip).
 //
 // Kernels
 //   pack_kv_kernel   K/V [token][kv head][d] -> per (kv head, 64-key sub-tile) images laid out
@@ -775,7 +775,8 @@ const char *sp_status_string(sp_status s) {
 }
 
 const char *sp_last_error(void) { return g_err; }
-
+// for the calls of the other translation unit
+__attribute__((visibility("hidden"))) void sp_set_error_text(const char *text) { set_err("%s", text); }
 
 sp_status sp_profile_enable(int32_t on) {
   g_err[0] = 0;
