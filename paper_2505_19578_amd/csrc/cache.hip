@@ -109,7 +109,7 @@ size_t plan_bytes(int32_t n) { return ((size_t)2 * n + 1) * sizeof(int32_t); }
 // Rows of a workgroup's tile, by the rows (group * max_new) that a request has under one KV head.
 int attn_tile_rows(const sp_step_shape *s, const sp_cache_shape *c) {
   const int64_t rows = (int64_t)s->max_new * (s->n_q_heads / c->n_kv_heads);
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 192;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
 }
 int64_t attn_most_keys(const sp_step_shape *s, const sp_cache_shape *c) { return (int64_t)s->max_pages * c->page_size; }
 int64_t attn_partial_rows(const sp_step_shape *s, const sp_cache_shape *c) {
@@ -160,10 +160,8 @@ sp_status launch_cache_attn(const CacheAttnParams &p, int tile_rows, int64_t ite
     hipLaunchKernelGGL((cache_attn_narrow_kernel<D, 2>), grid, block, 0, st, p);
   else if (tile_rows == 64)
     hipLaunchKernelGGL((cache_attn_wide_kernel<D, 1>), grid, block, 0, st, p);
-  else if (tile_rows == 128)
-    hipLaunchKernelGGL((cache_attn_wide_kernel<D, 2>), grid, block, 0, st, p);
   else
-    hipLaunchKernelGGL((cache_attn_wide_kernel<D, 3>), grid, block, 0, st, p);
+    hipLaunchKernelGGL((cache_attn_wide_kernel<D, 2>), grid, block, 0, st, p);
   const sp_status rc = launched("cache_attn_kernel");
   if (rc || cache_most_chunks(p.most_keys) == 1) return rc;  // no request has two chunks
   const int64_t rows = (int64_t)p.n_tok * p.hq;

@@ -22,6 +22,7 @@ namespace {
 // a request do not depend on what else the call holds.
 constexpr int CA_THREADS = 256, CA_WAVES = 4;
 constexpr float CA_SLACK = 8.0f;  // how far (log2) a row's maximum may outgrow its reference before the reference moves
+constexpr float CA_NONE = -3.0e38f;  // the reference of a row that has seen nothing: finite, so that 2^(-infinity - it) is 0
 
 struct CacheAttnParams {
   const uint16_t *q, *k, *v;
@@ -35,6 +36,14 @@ struct CacheAttnParams {
   int n_req, n_tok, hq, hk, group, page_shift, n_pages, width, words;
   float c;  // softmax scale * log2(e)
 };
+
+// The kernel's parameters once more from where they lie, for code that is rarely run: held in registers through the loops for its
+// sake they were spilled, and the loops reloaded others.  (Every kernel here has the struct as its only parameter.)
+__device__ __forceinline__ const CacheAttnParams &reloaded(const CacheAttnParams &) {
+  uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return *(const CacheAttnParams *)(const __attribute__((address_space(4))) CacheAttnParams *)at;
+}
 
 __device__ __forceinline__ int wave_prefix(int x, int lane) {  // inclusive
 #pragma unroll
@@ -159,7 +168,8 @@ struct CacheRows {
   static constexpr int KS = D / 32, DT = D / 16;  // k-steps of S^T, row tiles of O^T
   bf16x8 q[NC][KS];
   f32x4 o[NC][DT], ones[NC];
-  float m[NC], l[NC];
+  // reference (log2), what a product has to exceed to move it, sum of the weights
+  float m[NC], limit[NC], l[NC];
 
   __device__ __forceinline__ void begin(const CacheAttnParams &p, const CacheRequest &rq, int kvh, int row0, int g, int i) {
 #pragma unroll
@@ -177,7 +187,8 @@ struct CacheRows {
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[c][d] = f32x4{0.f, 0.f, 0.f, 0.f};
       ones[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m[c] = -INFINITY;
+      m[c] = CA_NONE;
+      limit[c] = -INFINITY;
       l[c] = 0.f;
     }
   }
@@ -188,52 +199,63 @@ struct CacheRows {
     const uint64_t *mask = p.words ? p.mask + (int64_t)(rq.s.first + t) * p.words : nullptr;
     return (cache_visible(kb, it.ctx, rq.s.fresh, t, mask, p.words) & there) >> (4 * g);
   }
-  // Weights of a step whose products are x (keys that are not seen: -infinity), as the B operand of the next product.
-  __device__ __forceinline__ void weigh(const f32x4 (&x)[2][NC], float scale, bf16x8 (&pf)[NC]) {
-    float top[NC];
-    bool grow = false;
+  // A step's products x (keys that are not seen: -infinity) in three parts: the largest of each column's, ..
+  __device__ __forceinline__ void largest(const f32x4 (&x)[2][NC], float (&top)[NC]) const {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      float t = fmaxf(fmaxf(x[0][c][0], x[0][c][1]), fmaxf(x[0][c][2], x[0][c][3]));
-      t = fmaxf(t, fmaxf(fmaxf(x[1][c][0], x[1][c][1]), fmaxf(x[1][c][2], x[1][c][3])));
-      top[c] = t * scale;
-      grow |= top[c] > m[c] + CA_SLACK;
+      const float t = fmaxf(fmaxf(x[0][c][0], x[0][c][1]), fmaxf(x[0][c][2], x[0][c][3]));
+      top[c] = fmaxf(t, fmaxf(fmaxf(x[1][c][0], x[1][c][1]), fmaxf(x[1][c][2], x[1][c][3])));
     }
-    if (any_lane(grow)) {  // rare: the reference only has to stay within 2^SLACK of the maximum
+  }
+  // .. the references, which only have to stay within 2^SLACK of the largest weight, so that they rarely move, ..
+  __device__ __forceinline__ void follow(const float (&top)[NC], float scale) {
+    bool grow = false;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float t = top[c];
-        t = fmaxf(t, __shfl_xor(t, 16));
-        t = fmaxf(t, __shfl_xor(t, 32));
-        const float to = t > m[c] + CA_SLACK ? t : m[c];
-        const float f = to == m[c] ? 1.f : __builtin_amdgcn_exp2f(m[c] - to);
+    for (int c = 0; c < NC; ++c) grow |= top[c] > limit[c];
+    if (!any_lane(grow)) return;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float t = top[c];
+      t = fmaxf(t, __shfl_xor(t, 16));
+      t = fmaxf(t, __shfl_xor(t, 32));
+      if (t > limit[c]) {
+        const float to = t * scale, f = __builtin_amdgcn_exp2f(m[c] - to);
         m[c] = to;
+        limit[c] = t + CA_SLACK / scale;
         l[c] *= f;
         ones[c] *= f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[c][d] *= f;
       }
     }
+  }
+  // .. and the weights, as the B operand of the next product.  They are rounded to bf16 for it (relative 2^-8 at most each).
+  // O is divided by the sum of the rounded ones, which the matrix pipe forms with a row of ones (add_ones), so a row that few
+  // keys dominate keeps no error of its sum; lse is that of the unrounded sum.
+  // (pairs of them: pairs[c][n] are weights 2 n and 2 n + 1 of column group c)
+  template <int FROM, int TO>
+  __device__ __forceinline__ void weigh_part(const f32x4 (&x)[2][NC], float scale, uint32_t (&pairs)[NC][4]) {
+    static_assert(FROM % 2 == 0 && TO % 2 == 0, "pairs");
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int e = FROM; e < TO; e += 2) {
+        const float y = __builtin_amdgcn_exp2f(x[e / 4][c][e % 4] * scale - m[c]);
+        const float z = __builtin_amdgcn_exp2f(x[e / 4][c][e % 4 + 1] * scale - m[c]);
+        l[c] += y;
+        l[c] += z;
+        pairs[c][e / 2] = pack_bf16(y, z);
+      }
+    }
+  }
+  static __device__ __forceinline__ bf16x8 weights_of(const uint32_t (&pairs)[4]) {
+    return __builtin_bit_cast(bf16x8, (u32x4{pairs[0], pairs[1], pairs[2], pairs[3]}));
+  }
+  __device__ __forceinline__ void add_ones(const bf16x8 (&pf)[NC]) {
     const uint32_t one2 = 0x3f803f80u;
     const bf16x8 all_ones = __builtin_bit_cast(bf16x8, (u32x4{one2, one2, one2, one2}));
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      float e[8];
-      const float ref = m[c] == -INFINITY ? 0.f : m[c];  // (nothing seen yet: weights are 2^-infinity)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          e[4 * j + r] = __builtin_amdgcn_exp2f(x[j][c][r] * scale - ref);
-          l[c] += e[4 * j + r];
-        }
-      // The weights are rounded to bf16 for the product (relative 2^-8 at most each).  O is divided by the sum of the rounded
-      // ones, which the matrix pipe forms with a row of ones, so a row that few keys dominate keeps no error of its sum;
-      // lse is that of the unrounded sum.
-      const u32x4 y = {pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7])};
-      pf[c] = __builtin_bit_cast(bf16x8, y);
-      ones[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all_ones, pf[c], ones[c], 0, 0, 0);
-    }
+    for (int c = 0; c < NC; ++c) ones[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all_ones, pf[c], ones[c], 0, 0, 0);
   }
   // O += V P, V's fragments as read(d) gives them
   template <class Read>
@@ -422,8 +444,15 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_narrow_kernel(CacheA
         odd_values = any_lane(odd);
       }
       store_v(vr);
+      float top[NC];
+      rows.largest(x, top);
+      rows.follow(top, p.c);
+      uint32_t pairs[NC][4];
+      rows.template weigh_part<0, 8>(x, p.c, pairs);
       bf16x8 pf[NC];
-      rows.weigh(x, p.c, pf);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) pf[c] = rows.weights_of(pairs[c]);
+      rows.add_ones(pf);
       if (!odd_values && s + 1 < steps) load_v(step_key(s + 1), id0, id1);
       rows.add_values(pf, v_fragment);
       if (odd_values) {
@@ -463,19 +492,19 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_narrow_kernel(CacheA
         float top = sm[0][16 * c + i];
 #pragma unroll
         for (int x = 1; x < CA_WAVES; ++x) top = fmaxf(top, sm[x][16 * c + i]);
-        const float f = rows.m[c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rows.m[c] - top);
+        const float f = rows.m[c] == CA_NONE ? 0.f : __builtin_amdgcn_exp2f(rows.m[c] - top);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
           *(f32x4 *)(sum + (w * 16 + i) * OROW + 16 * d + 4 * g) = f == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : rows.o[c][d] * f;
       }
       __syncthreads();
       const int row = it.tile * ROWS + 16 * c + orow;
-      float top = -INFINITY, ls = 0.f, lr = 0.f;
+      float top = CA_NONE, ls = 0.f, lr = 0.f;
 #pragma unroll
       for (int x = 0; x < CA_WAVES; ++x) top = fmaxf(top, sm[x][16 * c + orow]);
 #pragma unroll
       for (int x = 0; x < CA_WAVES; ++x) {
-        const float f = sm[x][16 * c + orow] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[x][16 * c + orow] - top);
+        const float f = sm[x][16 * c + orow] == CA_NONE ? 0.f : __builtin_amdgcn_exp2f(sm[x][16 * c + orow] - top);
         ls += f * sl[x][16 * c + orow];
         lr += f * sr[x][16 * c + orow];
       }
@@ -511,21 +540,51 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_narrow_kernel(CacheA
 }
 
 // ------------------------------------------------------------------------------------------------------------------ wide
-// One wavefront-wide 1 KiB copy from memory to LDS: lane l moves 16 bytes at g_uniform + lane_off to LDS byte address
-// lds_base + 16 l.  From inline assembly, so that the compiler does not wait for it at the next LDS read: the kernel counts these
-// loads itself (wait_copies), and the compiler's own waits, which count in order, only become stricter by them.
-__device__ __forceinline__ void copy_to_lds(const void *g_uniform, uint32_t lane_off, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(lane_off), "s"(g_uniform)
-               : "memory", "m0");
+// N wavefront-wide copies of 1 KiB from memory to LDS, lds_base and on: lane l of copy n moves 16 bytes at g_uniform + lane_off[n] +
+// 1024 n to LDS byte address lds_base + 1024 n + 16 l (the instruction's own offset moves both addresses).
+// From inline assembly, so that the compiler does not wait for them at the next LDS read: the kernel counts these loads itself
+// (wait_copies), and the compiler's own waits, which count in order, only become stricter by them.
+template <int N>
+__device__ __forceinline__ void copy_to_lds(const void *g_uniform, const uint32_t (&lane_off)[N], uint32_t lds_base) {
+  static_assert(N == 1 || N == 2, "one setting of M0");
+  if constexpr (N == 1)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(lane_off[0]), "s"(g_uniform)
+                 : "memory", "m0");
+  else
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds_base),
+        "v"(lane_off[0]), "v"(lane_off[1]), "s"(g_uniform)
+        : "memory", "m0");
 }
 template <int N>
 __device__ __forceinline__ void wait_copies() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// Steps of 32 keys of K and V lie in a ring in LDS, filled RING - 1 steps ahead by copies that pass no registers; one barrier a
-// step.  A row's 16-byte pieces lie XOR-swizzled by the row number, so that the fragments' reads (16 rows at a time for K, four
+// Steps of 32 keys of K and V lie in a ring in LDS, filled two steps ahead by copies that pass no registers; one barrier a step.
+// A row's 16-byte pieces lie XOR-swizzled by the row number, so that the fragments' reads (16 rows at a time for K, four
 // rows for V) meet no bank twice; the copies' lanes fetch the pieces in that order.
+//
+// Step s: the matrix pipe takes S of step s + 1, then O += V P of step s; beside it the vector unit makes the weights of step s,
+// then the largest of S of step s + 1.
+//
+// N products groups, group n with the fragment that read(n) names: use(n, fragment) issues it and its share of the vector work.
+// AHEAD fragments are on their way before the first group and one more goes out with each, in this order (the fences): left to
+// itself the compiler keeps one fragment at a time and has every group wait for a read of its own.
+template <int N, class Read, class Use>
+__device__ __forceinline__ void groups_read_ahead(Read &&read, Use &&use) {
+  constexpr int AHEAD = N < 4 ? N : 4;
+  bf16x8 fr[AHEAD + 1];
+  static_for<0, AHEAD>([&](auto nc) __attribute__((always_inline)) { fr[decltype(nc)::value] = read(decltype(nc)::value); });
+  __builtin_amdgcn_sched_barrier(0);
+  static_for<0, N>([&](auto nc) __attribute__((always_inline)) {
+    constexpr int n = decltype(nc)::value;
+    if constexpr (n + AHEAD < N) fr[(n + AHEAD) % (AHEAD + 1)] = read(n + AHEAD);
+    use(nc, fr[n % (AHEAD + 1)]);
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+
 template <int D, int NC>
 __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAttnParams p) {
   constexpr int WROWS = 16 * NC, ROWS = CA_WAVES * WROWS;
@@ -541,23 +600,30 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, i = lane & 15;
   const int w = uniform(tid >> 6);
-  // byte of piece x of row r of a tile
-  auto place = [](int r, int x) { return r * ROWB + ((x ^ (D == 128 ? r & 15 : (r >> 1) & 7)) * 16); };
+  auto swizzle = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
   // this lane's part of copy n: row and piece (the LDS side is lane after lane)
   uint32_t copy_off[COPIES];
 #pragma unroll
   for (int n = 0; n < COPIES; ++n) {
-    const int r = (CACHE_STEP / CA_WAVES) * w + COPY_ROWS * n + lane / PIECES, slot = lane % PIECES;
-    const int x = slot ^ (D == 128 ? r & 15 : (r >> 1) & 7);
-    copy_off[n] = 2u * (uint32_t)((r & 15) * (int)p.c_st + 8 * x);
+    const int r = (CACHE_STEP / CA_WAVES) * w + COPY_ROWS * n + lane / PIECES;
+    // (rows are at least D elements apart, so 1024 n, which the instruction adds, never exceeds row COPY_ROWS * n's begin)
+    copy_off[n] = 2u * (uint32_t)((r & 15) * (int)p.c_st + 8 * ((lane % PIECES) ^ swizzle(r))) - 1024u * n;
   }
-  auto k_fragment = [&](const char *tile, int j, int s) -> bf16x8 {
-    return *(const bf16x8 *)(tile + place(16 * j + i, 4 * s + g));
+  // byte of this lane's part of the first fragments (in slot 0); the others' are XORs of it, as pieces are numbered from 0 in a row
+  const uint32_t k_lane = lds0 + (uint32_t)(i * ROWB + 16 * (g ^ swizzle(i)));
+  const int v_row = 4 * g + (i >> 2);
+  const uint32_t v_lane = lds0 + (uint32_t)(v_row * ROWB + 16 * (((i & 3) >> 1) ^ swizzle(v_row)) + 8 * (i & 1));
+  typedef __attribute__((address_space(3))) const bf16x8 *lds_bf16x8;
+  auto k_fragment = [&](uint32_t slot, int j, int y) -> bf16x8 {
+    return *(lds_bf16x8)(((slot + k_lane) ^ (64 * y)) + 16 * ROWB * j);
   };
-  auto v_fragment = [&](char *tile, int d) -> bf16x8 {
-    const int r = 4 * g + (i >> 2), x = 2 * d + ((i & 3) >> 1), half = (i & 1) * 8;
-    return read_transposed(tile + place(r, x) + half, tile + place(r + 16, x) + half);
+  auto v_fragment = [&](uint32_t slot, int d) -> bf16x8 {
+    const uint32_t at = ((slot + v_lane) ^ (32 * d)) + TILE;
+    const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)at);
+    const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(at + 16 * ROWB));
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   };
+  auto after = [](uint32_t slot) { return (slot + 2 * TILE) & (RING * 2 * TILE - 1); };
 
   CacheWalk<ROWS> walk(p, lane);
   CacheRequest rq;
@@ -566,118 +632,167 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
     CacheRows<D, NC> rows;
     const int row0 = it.tile * ROWS + w * WROWS;
     rows.begin(p, rq, it.kvh, row0, g, i);
-    const int32_t *row_pages = p.table + (int64_t)rq.r * p.width;
     const int steps = it.k_begin < it.k_end ? (it.k_end - it.k_begin + CACHE_STEP - 1) / CACHE_STEP : 0;
-    // pages of 64 steps at a time: lane s holds those of both halves of step s; -1: no such key, or a page that does not exist
-    int half0 = -1, half1 = -1, pages_from = 0;
-    auto page_at = [&](int key) {
+    // All keys of a step before `soft` lie in the context and on pages that exist: every row sees them.
+    int soft = it.ctx > it.k_begin ? (it.ctx - it.k_begin) / CACHE_STEP : 0;
+    auto page_at = [&](const CacheAttnParams &c, int key) {
       if (key >= it.k_end) return -1;
-      const int id = row_pages[key >> p.page_shift];
-      return id >= 0 && id < p.n_pages ? id : -1;
+      const int id = c.table[(int64_t)rq.r * c.width + (key >> c.page_shift)];
+      return id >= 0 && id < c.n_pages ? id : -1;
     };
-    auto load_pages = [&](int s0) {
-      const int key = it.k_begin + CACHE_STEP * (s0 + lane);
-      half0 = page_at(key);
-      half1 = page_at(key + 16);
-      pages_from = s0;
+    // Places of this wavefront's half of 64 steps at a time, lane s those of step s, in bytes from the cache's begin.  Keys that do
+    // not exist or lie on no page are read from page 0; they count for nothing.
+    uint32_t from_low = 0, from_high = 0;
+    int from_step = 0;
+    auto load_places = [&](int s0) {
+      const CacheAttnParams &c = reloaded(p);
+      const int key = it.k_begin + CACHE_STEP * (s0 + lane), mine = key + 16 * (w >> 1);
+      const int a = page_at(c, key), b = page_at(c, key + 16), id = w >> 1 ? b : a;
+      const uint64_t none = __builtin_amdgcn_ballot_w64(key < it.k_end && (a < 0 || (b < 0 && key + 16 < it.k_end)));
+      if (none) soft = min(soft, s0 + (int)__builtin_ctzll(none));
+      const uint64_t at = 2 * ((uint64_t)(id < 0 ? 0 : id) * (uint64_t)c.c_sp +
+                               (uint64_t)(mine & ((1 << c.page_shift) - 1)) * (uint64_t)c.c_st + (uint64_t)it.kvh * (uint64_t)c.c_sh);
+      from_low = (uint32_t)at, from_high = (uint32_t)(at >> 32);
+      from_step = s0;
     };
-    const int64_t head_off = (int64_t)it.kvh * p.c_sh;
-    uint64_t bad = 0;  // of the steps in the ring, two bits each (step s: bits 2 (s % 32)): a half without a page
+    uint32_t fill = 0;  // the slot that the next fetch fills
     auto fetch = [&](int s) {
-      if (s - pages_from >= 64) load_pages(s);
-      const int a = __builtin_amdgcn_readlane(half0, s - pages_from), b = __builtin_amdgcn_readlane(half1, s - pages_from);
-      const int at = 2 * (s & 31);
-      bad = (bad & ~(3ull << at)) | ((uint64_t)((a < 0 ? 1 : 0) | (b < 0 ? 2 : 0)) << at);
-      const int half = w >> 1, id = half ? b : a, key = it.k_begin + CACHE_STEP * s + 16 * half;
-      const int64_t from = (int64_t)(id < 0 ? 0 : id) * p.c_sp + (int64_t)(key & ((1 << p.page_shift) - 1)) * p.c_st + head_off;
-      const uint32_t to = lds0 + (uint32_t)((s % RING) * 2 * TILE + (CACHE_STEP / CA_WAVES) * w * ROWB);
-#pragma unroll
-      for (int n = 0; n < COPIES; ++n) copy_to_lds(p.k + from, copy_off[n], to + 1024 * n);
-#pragma unroll
-      for (int n = 0; n < COPIES; ++n) copy_to_lds(p.v + from, copy_off[n], to + TILE + 1024 * n);
+      if (s - from_step >= 64) load_places(s);
+      const uint64_t at = (uint32_t)__builtin_amdgcn_readlane(from_low, s - from_step) |
+                          (uint64_t)(uint32_t)__builtin_amdgcn_readlane(from_high, s - from_step) << 32;
+      const uint32_t to = lds0 + fill + (uint32_t)((CACHE_STEP / CA_WAVES) * w * ROWB);
+      copy_to_lds<COPIES>((const char *)p.k + at, copy_off, to);
+      copy_to_lds<COPIES>((const char *)p.v + at, copy_off, to + TILE);
+      fill = after(fill);
     };
-    if (steps > 0) load_pages(0);
-    for (int s = 0; s < RING - 1 && s < steps; ++s) fetch(s);
-    for (int s = 0; s < steps; ++s) {
-      if (s + RING - 2 < steps)
-        wait_copies<(RING - 2) * 2 * COPIES>();
+    // S^T of a step into `next`, and beside it beside(n) for n = 0 .. 2 KS - 1
+    auto products = [&](uint32_t slot, f32x4 (&next)[2][NC], auto &&beside) __attribute__((always_inline)) {
+      groups_read_ahead<2 * KS>([&](int n) { return k_fragment(slot, n / KS, n % KS); },
+                                [&](auto nc, const bf16x8 &a) __attribute__((always_inline)) {
+        constexpr int n = decltype(nc)::value, j = n / KS, y = n % KS;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          next[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, rows.q[c][y], y ? next[j][c] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+        beside(nc);
+      });
+    };
+    // what the rows see of step s that is not before `soft`
+    auto there = [&](const CacheAttnParams &c, int kb) {
+      return (page_at(c, kb) < 0 ? 0u : 0xffffu) | (page_at(c, kb + 16) < 0 ? 0u : 0xffff0000u);
+    };
+    auto hide = [&](int s, f32x4 (&x)[2][NC]) __attribute__((always_inline)) {
+      const CacheAttnParams &cp = reloaded(p);
+      const int kb = it.k_begin + CACHE_STEP * s;
+      const uint32_t exist = there(cp, kb);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const uint32_t see = rows.sees(cp, rq, it, row0 + 16 * c + i, kb, exist, g);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (!((see >> (16 * j + r)) & 1)) x[j][c][r] = -INFINITY;
+      }
+    };
+    // Values of such a step: those of keys that do not exist become zeros; those that are not finite are kept out of the product
+    // and added here to the rows that see them.
+    auto clean_values = [&](int s, uint32_t slot) __attribute__((always_inline)) {
+      constexpr int OWN = TILE / 16 / CA_THREADS;  // pieces of V that are this thread's to look at
+      const CacheAttnParams &cp = reloaded(p);
+      char *const vt = smem + slot + TILE;
+      const int kb = it.k_begin + CACHE_STEP * s;
+      const uint32_t exist = there(cp, kb);
+      int odd = 0;
+#pragma unroll
+      for (int n = 0; n < OWN; ++n) {
+        const int at = (n * CA_THREADS + tid) * 16, r = at / ROWB;
+        const u32x4 y = *(const u32x4 *)(vt + at);
+        if (kb + r >= it.k_end || !((exist >> r) & 1))
+          *(u32x4 *)(vt + at) = u32x4{0, 0, 0, 0};
+        else
+          odd |= odd_bf16x2(y[0]) || odd_bf16x2(y[1]) || odd_bf16x2(y[2]) || odd_bf16x2(y[3]);
+      }
+      if (!__syncthreads_or(odd)) return;
+      bf16x8 seen[NC];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) seen[c] = rows.as_ones(rows.sees(cp, rq, it, row0 + 16 * c + i, kb, exist, g));
+      u32x4 keep[OWN];
+#pragma unroll
+      for (int n = 0; n < OWN; ++n) keep[n] = *(const u32x4 *)(vt + (n * CA_THREADS + tid) * 16);
+#pragma unroll 1
+      for (int kind = 0; kind <= ODD_KINDS; ++kind) {  // the last round leaves the finite values
+#pragma unroll
+        for (int n = 0; n < OWN; ++n) {
+          u32x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = kind == ODD_KINDS ? without_odd(keep[n][e]) : ones_of_kind(keep[n][e], kind);
+          *(u32x4 *)(vt + (n * CA_THREADS + tid) * 16) = y;
+        }
+        __syncthreads();
+        if (kind == ODD_KINDS) break;
+        rows.add_kind(seen, kind, [&](int d) { return v_fragment(slot, d); });
+        __syncthreads();
+      }
+    };
+    float top[NC];
+    uint32_t slot = 0;  // of the present step
+    auto step = [&](int s, f32x4 (&x)[2][NC], f32x4 (&next)[2][NC]) __attribute__((always_inline)) {
+      // step s + 1 has arrived (step s + 2 may be on its way), and nobody reads step s - 1 any more
+      if (s + 2 < steps)
+        wait_copies<2 * COPIES>();
       else
         wait_copies<0>();
       __syncthreads();
-      const int gone = (int)((bad >> (2 * (s & 31))) & 3);
       if (s + RING - 1 < steps) fetch(s + RING - 1);
-      char *const kt = smem + (s % RING) * 2 * TILE, *const vt = kt + TILE;
-      const int kb = it.k_begin + CACHE_STEP * s;
-      f32x4 x[2][NC];
+      rows.follow(top, p.c);
+      uint32_t pairs[NC][4];
+      // (behind the last step: the products of whatever lies there, for nobody)
+      products(after(slot), next, [&](auto nc) __attribute__((always_inline)) {
+        constexpr int n = decltype(nc)::value, each = 16 / (2 * KS);  // of 8 weights, an even number every other group
+        if constexpr (each >= 4)
+          rows.template weigh_part<each / 2 * n, each / 2 *(n + 1)>(x, p.c, pairs);
+        else if constexpr (n % 2 == 0)
+          rows.template weigh_part<n, n + 2>(x, p.c, pairs);
+      });
+      bf16x8 pf[NC];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-#pragma unroll
-        for (int c = 0; c < NC; ++c) x[j][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int y = 0; y < KS; ++y) {
-          const bf16x8 a = k_fragment(kt, j, y);
-#pragma unroll
-          for (int c = 0; c < NC; ++c) x[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, rows.q[c][y], x[j][c], 0, 0, 0);
-        }
+      for (int c = 0; c < NC; ++c) {
+        asm volatile("" : "+v"(pairs[c][0]), "+v"(pairs[c][1]), "+v"(pairs[c][2]), "+v"(pairs[c][3]));  // made here, not where they are used
+        pf[c] = rows.weights_of(pairs[c]);
       }
-      const bool whole = kb + CACHE_STEP <= it.ctx && !gone;
-      const uint32_t there = (gone & 1 ? 0u : 0xffffu) | (gone & 2 ? 0u : 0xffff0000u);
-      bool odd_values = false;
-      // values of keys that do not exist become zeros; values that are not finite are kept out of the product and added to the
-      // rows that see them
-      constexpr int OWN = TILE / 16 / CA_THREADS;  // pieces of V that are this thread's to look at
-      auto no_value = [&](int at) {
-        const int r = at / ROWB;
-        return kb + r >= it.k_end || ((r < 16 ? gone : gone >> 1) & 1);
-      };
-      if (!whole) {
+      if (s + 1 >= soft) {
+        hide(s + 1, next);
+        if (s >= soft) clean_values(s, slot);
+      }
+      rows.add_ones(pf);
+      groups_read_ahead<DT>([&](int d) { return v_fragment(slot, d); },
+                            [&](auto dc, const bf16x8 &a) __attribute__((always_inline)) {
+        constexpr int d = decltype(dc)::value;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const uint32_t see = rows.sees(p, rq, it, row0 + 16 * c + i, kb, there, g);
+          rows.o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf[c], rows.o[c][d], 0, 0, 0);
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (!((see >> (16 * j + r)) & 1)) x[j][c][r] = -INFINITY;
+          for (int e = 8 / DT * d; e < 8 / DT * (d + 1); ++e) top[c] = e ? fmaxf(top[c], next[e / 4][c][e % 4]) : next[0][c][0];
         }
-        int odd = 0;
-#pragma unroll
-        for (int n = 0; n < OWN; ++n) {
-          const int at = (n * CA_THREADS + tid) * 16;
-          const u32x4 y = *(const u32x4 *)(vt + at);
-          if (no_value(at))
-            *(u32x4 *)(vt + at) = u32x4{0, 0, 0, 0};
-          else
-            odd |= odd_bf16x2(y[0]) || odd_bf16x2(y[1]) || odd_bf16x2(y[2]) || odd_bf16x2(y[3]);
-        }
-        odd_values = __syncthreads_or(odd) != 0;
+      });
+      slot = after(slot);
+    };
+    if (steps > 0) {
+      load_places(0);
+      for (int s = 0; s < RING - 1 && s < steps; ++s) fetch(s);
+      f32x4 even[2][NC], odd[2][NC];
+      if (steps > 2)
+        wait_copies<2 * 2 * COPIES>();
+      else
+        wait_copies<0>();
+      __syncthreads();
+      products(0, even, [](auto) {});
+      if (0 >= soft) hide(0, even);
+      rows.largest(even, top);
+      for (int s = 0; s < steps; s += 2) {
+        step(s, even, odd);
+        if (s + 1 < steps) step(s + 1, odd, even);
       }
-      bf16x8 pf[NC];
-      rows.weigh(x, p.c, pf);
-      if (odd_values) {
-        bf16x8 seen[NC];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) seen[c] = rows.as_ones(rows.sees(p, rq, it, row0 + 16 * c + i, kb, there, g));
-        u32x4 keep[OWN];
-#pragma unroll
-        for (int n = 0; n < OWN; ++n) keep[n] = *(const u32x4 *)(vt + (n * CA_THREADS + tid) * 16);
-#pragma unroll 1
-        for (int kind = 0; kind <= ODD_KINDS; ++kind) {  // the last round leaves the finite values
-#pragma unroll
-          for (int n = 0; n < OWN; ++n) {
-            u32x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = kind == ODD_KINDS ? without_odd(keep[n][e]) : ones_of_kind(keep[n][e], kind);
-            *(u32x4 *)(vt + (n * CA_THREADS + tid) * 16) = y;
-          }
-          __syncthreads();
-          if (kind < ODD_KINDS) {
-            rows.add_kind(seen, kind, [&](int d) { return v_fragment(vt, d); });
-            __syncthreads();
-          }
-        }
-      }
-      rows.add_values(pf, [&](int d) { return v_fragment(vt, d); });
     }
     rows.finish();
 #pragma unroll
@@ -721,7 +836,7 @@ __global__ __launch_bounds__(CA_THREADS) void cache_join_kernel(CacheAttnParams 
   const int kvh = hq / p.group, row = (token - rq.s.first) * p.group + hq - kvh * p.group;
   const int64_t from = partial_row(rq, kvh, row, 0);
   const int chunks = rq.s.chunks;
-  float top = -INFINITY;
+  float top = CA_NONE;
   for (int c = lane; c < chunks; c += 64) top = fmaxf(top, p.part_ml[(from + c) * 4]);
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
@@ -730,9 +845,9 @@ __global__ __launch_bounds__(CA_THREADS) void cache_join_kernel(CacheAttnParams 
   for (int e = 0; e < E; ++e) y[e] = 0.f;
   for (int c0 = 0; c0 < chunks; c0 += 64) {
     const int n = min(64, chunks - c0);
-    f32x4 ml = {-INFINITY, 0.f, 0.f, 0.f};
+    f32x4 ml = {CA_NONE, 0.f, 0.f, 0.f};
     if (lane < n) ml = *(const f32x4 *)(p.part_ml + (from + c0 + lane) * 4);
-    const float f = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
+    const float f = ml[0] == CA_NONE ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
     ls += f * ml[1];
     lr += f * ml[2];
     const float *src = p.part_o + (from + c0) * D + E * lane;

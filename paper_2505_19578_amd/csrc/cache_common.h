@@ -18,6 +18,15 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
+// f(integral_constant<int, G>) for G = FROM .. TO-1, expanded at compile time
+template <int FROM, int TO, class F>
+__device__ __forceinline__ void static_for(F &&f) {
+  if constexpr (FROM < TO) {
+    f(std::integral_constant<int, FROM>{});
+    static_for<FROM + 1, TO>(f);
+  }
+}
+
 __device__ __forceinline__ float bf_lo(uint32_t x) { return __builtin_bit_cast(float, x << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // round to nearest, ties to even

@@ -63,11 +63,11 @@ struct CacheShare {
   int32_t first, fresh, keys, rows, tiles, units, chunks;
 };
 // Units of a chunk.  It goes by the request's own sizes alone, so that a request's result is the same bits whatever else the
-// call holds: about 16 chunks per 64 rows, so that one request spreads over the chip, of 2 to 16 units per 64 rows, so that a
+// call holds: about 16 chunks per 64 rows, so that one request spreads over the chip, of 2 to 8 units per 64 rows, so that a
 // workgroup has enough to do and a long context still makes more workgroups than 16.
 constexpr int64_t cache_chunk_units(int64_t units, int64_t rows) {
   const int64_t t = (rows + 63) / 64, u = (units * t + 15) / 16;
-  return u < 2 ? 2 : u > 16 * t ? 16 * t : u;
+  return u < 2 ? 2 : u > 8 * t ? 8 * t : u;
 }
 // Tokens and keys come from device memory: whatever is in it, a share is a share of rows and keys that exist.
 constexpr CacheShare cache_share(int64_t first, int64_t end, int64_t keys, int64_t n_tokens, int64_t most_keys, int group, int tile_rows) {
@@ -89,7 +89,7 @@ constexpr CacheShare cache_share(int64_t first, int64_t end, int64_t keys, int64
 // chunks <= most / t + 1 with t = ceil(rows / 64) and `most` as follows
 constexpr int64_t cache_most_chunks(int64_t most_keys) {
   const int64_t units = (most_keys + CACHE_UNIT - 1) / CACHE_UNIT;
-  return units <= 2 ? 1 : units / 16 > 16 ? (units + 15) / 16 : 16;
+  return units <= 2 ? 1 : units / 8 > 16 ? (units + 7) / 8 : 16;
 }
 // rows of partial results: rows * chunks
 constexpr int64_t cache_partial_rows(int64_t n_requests, int64_t n_tokens, int group, int64_t most_keys) {
