@@ -82,13 +82,17 @@ def _rows(t, shape, strides, device: int, name: str):
     return t.data_ptr()
 
 
+# The current stream's handle without a Stream object around it: 0.06 us of a call's 9 instead of 2.5.
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _call(fn, device: int, *args):
     """fn(*args, stream) on the current stream of `device`."""
     if device == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+        _check(fn(*args, _stream_of(device)))
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+            _check(fn(*args, _stream_of(device)))
 
 
 def cache_shape_of(cache) -> SpCacheShape:

@@ -100,9 +100,6 @@ sp_status check_cache(const sp_cache_shape *c) {
 int log2_of(int32_t x) { return __builtin_ctz((unsigned)x); }
 
 // ------------------------------------------------------------------------------------------------------------------ plan
-// Tokens up to which one workgroup makes the whole plan: it takes a launch less.
-constexpr int PLAN_ONE_LAUNCH = 4096;
-
 size_t plan_bytes(int32_t n) { return ((size_t)2 * n + 1) * sizeof(int32_t); }
 
 // ------------------------------------------------------------------------------------------------------------- attention
@@ -217,15 +214,14 @@ sp_status sp_cache_plan(int32_t n_requests, int32_t max_tokens, int32_t page_siz
   p.table = block_table, p.held_out = n_held_out, p.n_free_out = n_free_out, p.tok_start = tok_start, p.seq_len = seq_len;
   p.positions = positions, p.slots = slots, p.status = status, p.mask = tree_mask;
   p.old_held = (int32_t *)workspace, p.page_start = p.old_held + n_requests, p.free_count = p.page_start + n_requests;
-  p.n = n_requests, p.max_tokens = max_tokens, p.page = page_size, p.width = max_pages, p.words = mask_words;
+  p.n = n_requests, p.max_tokens = max_tokens, p.page_shift = log2_of(page_size), p.width = max_pages, p.words = mask_words;
   p.free_capacity = free_capacity;
   hipStream_t st = (hipStream_t)hip_stream;
   const bool one = max_tokens <= PLAN_ONE_LAUNCH;
   hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, p, one ? 1 : 0);
   if ((rc = launched("plan_kernel")) || one) return rc;
-  const int token_blocks = std::min((max_tokens + PLAN_PART_THREADS - 1) / PLAN_PART_THREADS, 2048);
-  const int tree_blocks = parents ? (n_requests + PLAN_PART_THREADS / 64 - 1) / (PLAN_PART_THREADS / 64) : 0;
-  hipLaunchKernelGGL(plan_tokens_kernel, dim3((unsigned)(token_blocks + tree_blocks)), dim3(PLAN_PART_THREADS), 0, st, p, token_blocks);
+  hipLaunchKernelGGL(plan_tokens_kernel, dim3((unsigned)((max_tokens + PLAN_PART_TOKENS - 1) / PLAN_PART_TOKENS)), dim3(PLAN_PART_THREADS),
+                     0, st, p);
   return launched("plan_tokens_kernel");
 }
 
@@ -320,7 +316,7 @@ sp_status sp_cache_attn(const sp_step_shape *shape, const sp_cache_shape *cache,
   p.part_o = (float *)workspace, p.part_ml = p.part_o + (size_t)attn_partial_rows(shape, cache) * c.head_dim;
   p.q_st = s.q_stride_t, p.q_sh = s.q_stride_h, p.o_st = s.o_stride_t, p.o_sh = s.o_stride_h;
   p.c_sp = c.stride_page, p.c_st = c.stride_token, p.c_sh = c.stride_head;
-  p.most_keys = attn_most_keys(shape, cache);
+  p.most_keys = (int)attn_most_keys(shape, cache);
   p.n_req = s.n_requests, p.n_tok = s.n_tokens, p.hq = s.n_q_heads, p.hk = c.n_kv_heads, p.group = s.n_q_heads / c.n_kv_heads;
   p.page_shift = log2_of(c.page_size), p.n_pages = c.n_pages, p.width = s.max_pages, p.words = s.mask_words;
   const float scale = s.softmax_scale > 0.f ? s.softmax_scale : 1.0f / sqrtf((float)c.head_dim);

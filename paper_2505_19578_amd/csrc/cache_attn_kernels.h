@@ -32,7 +32,7 @@ struct CacheAttnParams {
   const uint64_t *mask;
   float *part_o, *part_ml;  // [partial rows][D], [partial rows][4]: reference, sum, sum of rounded weights
   int64_t q_st, q_sh, o_st, o_sh, c_sp, c_st, c_sh;
-  int64_t most_keys;
+  int most_keys;
   int n_req, n_tok, hq, hk, group, page_shift, n_pages, width, words;
   float c;  // softmax scale * log2(e)
 };
@@ -43,15 +43,6 @@ __device__ __forceinline__ const CacheAttnParams &reloaded(const CacheAttnParams
   uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(at));
   return *(const CacheAttnParams *)(const __attribute__((address_space(4))) CacheAttnParams *)at;
-}
-
-__device__ __forceinline__ int wave_prefix(int x, int lane) {  // inclusive
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
 }
 
 // A request as the workgroups of a call see it.
@@ -78,8 +69,8 @@ struct CacheWalk {
     first = live ? p.start[r] : 0, end = live ? p.start[r + 1] : 0, keys = live ? p.seq[r] : 0;
     const CacheShare s = cache_share(first, end, keys, p.n_tok, p.most_keys, p.group, TILE);
     good = !any_lane(end < first);  // otherwise this is no tok_start: nothing behind is done, so that no index leaves its buffer
-    upto = items + wave_prefix(s.tiles * p.hk * s.chunks, lane);
-    parts = rows + wave_prefix(s.chunks > 1 ? s.rows * p.hk * s.chunks : 0, lane);
+    upto = items + (int)wave_prefix((uint32_t)(s.tiles * p.hk * s.chunks));
+    parts = rows + (int)wave_prefix((uint32_t)(s.chunks > 1 ? s.rows * p.hk * s.chunks : 0));
   }
   template <class Test>
   __device__ __forceinline__ bool seek(Test &&test, CacheRequest &out) {
@@ -119,10 +110,10 @@ struct CacheItem {
 __device__ __forceinline__ CacheItem item_of(const CacheRequest &rq, int index, int hk) {
   const CachePlace place = cache_place(index - rq.items_before, rq.s.chunks * hk, rq.s.tiles);
   CacheItem it;
-  it.chunk = place.pair / hk;
+  it.chunk = (int)((uint32_t)place.pair / (uint32_t)hk);
   it.kvh = place.pair - it.chunk * hk;
   it.tile = place.tile;
-  const int per = (rq.s.units + rq.s.chunks - 1) / rq.s.chunks;
+  const int per = (int)((uint32_t)(rq.s.units + rq.s.chunks - 1) / (uint32_t)rq.s.chunks);
   it.k_begin = it.chunk * per * CACHE_UNIT;
   it.k_end = min(rq.s.keys, it.k_begin + per * CACHE_UNIT);
   it.ctx = rq.s.keys - rq.s.fresh;
@@ -176,7 +167,7 @@ struct CacheRows {
     for (int c = 0; c < NC; ++c) {
       const int row = row0 + 16 * c + i;
       const bool live = row < rq.s.rows;
-      const int t = live ? row / p.group : 0, hq = kvh * p.group + (live ? row - t * p.group : 0);
+      const int t = live ? (int)((uint32_t)row / (uint32_t)p.group) : 0, hq = kvh * p.group + (live ? row - t * p.group : 0);
       const uint16_t *src = p.q + (int64_t)(rq.s.first + t) * p.q_st + (int64_t)hq * p.q_sh + 8 * g;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -195,7 +186,7 @@ struct CacheRows {
   // bits of the step's keys that a row sees, from key 4 g of each half on (bits 0 .. 3 and 16 .. 19)
   static __device__ __forceinline__ uint32_t sees(const CacheAttnParams &p, const CacheRequest &rq, const CacheItem &it, int row,
                                                   int kb, uint32_t there, int g) {
-    const int t = row < rq.s.rows ? row / p.group : 0;
+    const int t = row < rq.s.rows ? (int)((uint32_t)row / (uint32_t)p.group) : 0;
     const uint64_t *mask = p.words ? p.mask + (int64_t)(rq.s.first + t) * p.words : nullptr;
     return (cache_visible(kb, it.ctx, rq.s.fresh, t, mask, p.words) & there) >> (4 * g);
   }
@@ -526,7 +517,7 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_narrow_kernel(CacheA
         for (int e = 0; e < E; e += 4) *(f32x4 *)(p.part_o + at * D + E * piece + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
         if (piece == 0) *(f32x4 *)(p.part_ml + at * 4) = f32x4{top, ls, lr, 0.f};
       } else {
-        const int t = row / p.group, hq = it.kvh * p.group + row - t * p.group;
+        const int t = (int)((uint32_t)row / (uint32_t)p.group), hq = it.kvh * p.group + row - t * p.group;
         const float inv = inverse(lr);
         uint16_t *dst = p.o + (int64_t)(rq.s.first + t) * p.o_st + (int64_t)hq * p.o_sh + E * piece;
 #pragma unroll
@@ -561,9 +552,9 @@ __device__ __forceinline__ void wait_copies() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// Steps of 32 keys of K and V lie in a ring in LDS, filled two steps ahead by copies that pass no registers; one barrier a step.
-// A row's 16-byte pieces lie XOR-swizzled by the row number, so that the fragments' reads (16 rows at a time for K, four
-// rows for V) meet no bank twice; the copies' lanes fetch the pieces in that order.
+// Steps of 32 keys lie in LDS, four of K and four of V in rings, filled two steps ahead by copies that pass no registers; one
+// barrier for two steps.  A row's 16-byte pieces lie XOR-swizzled by the row number, so that the fragments' reads (16 rows at a time
+// for K, four rows for V) meet no bank twice; the copies' lanes fetch the pieces in that order.
 //
 // Step s: the matrix pipe takes S of step s + 1, then O += V P of step s; beside it the vector unit makes the weights of step s,
 // then the largest of S of step s + 1.
@@ -595,7 +586,7 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
   constexpr int PIECES = ROWB / 16;             // 16-byte pieces of a row
   constexpr int COPY_ROWS = 1024 / ROWB;        // rows that one copy moves
   constexpr int COPIES = CACHE_STEP / CA_WAVES / COPY_ROWS;  // copies of a wavefront for its 8 rows of K (and as many for V)
-  __shared__ __attribute__((aligned(1024))) char smem[RING * 2 * TILE];
+  __shared__ __attribute__((aligned(1024))) char smem[RING * 2 * TILE];  // slot n: K of a step, then V of a step
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) char *)smem;
 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, i = lane & 15;
@@ -623,7 +614,7 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
     const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(at + 16 * ROWB));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  auto after = [](uint32_t slot) { return (slot + 2 * TILE) & (RING * 2 * TILE - 1); };
+  auto slot_of = [](int s) { return (uint32_t)(s % RING) * (2 * TILE); };
 
   CacheWalk<ROWS> walk(p, lane);
   CacheRequest rq;
@@ -655,16 +646,13 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
       from_low = (uint32_t)at, from_high = (uint32_t)(at >> 32);
       from_step = s0;
     };
-    uint32_t fill = 0;  // the slot that the next fetch fills
-    auto fetch = [&](int s) {
-      if (s - from_step >= 64) load_places(s);
-      const uint64_t at = (uint32_t)__builtin_amdgcn_readlane(from_low, s - from_step) |
-                          (uint64_t)(uint32_t)__builtin_amdgcn_readlane(from_high, s - from_step) << 32;
-      const uint32_t to = lds0 + fill + (uint32_t)((CACHE_STEP / CA_WAVES) * w * ROWB);
-      copy_to_lds<COPIES>((const char *)p.k + at, copy_off, to);
-      copy_to_lds<COPIES>((const char *)p.v + at, copy_off, to + TILE);
-      fill = after(fill);
+    auto place_of = [&](int s) {
+      return (uint32_t)__builtin_amdgcn_readlane(from_low, s - from_step) |
+             (uint64_t)(uint32_t)__builtin_amdgcn_readlane(from_high, s - from_step) << 32;
     };
+    const uint32_t own_rows = lds0 + (uint32_t)((CACHE_STEP / CA_WAVES) * w * ROWB);
+    auto fetch_k = [&](int s) { copy_to_lds<COPIES>((const char *)p.k + place_of(s), copy_off, own_rows + slot_of(s)); };
+    auto fetch_v = [&](int s) { copy_to_lds<COPIES>((const char *)p.v + place_of(s), copy_off, own_rows + slot_of(s) + TILE); };
     // S^T of a step into `next`, and beside it beside(n) for n = 0 .. 2 KS - 1
     auto products = [&](uint32_t slot, f32x4 (&next)[2][NC], auto &&beside) __attribute__((always_inline)) {
       groups_read_ahead<2 * KS>([&](int n) { return k_fragment(slot, n / KS, n % KS); },
@@ -735,19 +723,11 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
       }
     };
     float top[NC];
-    uint32_t slot = 0;  // of the present step
     auto step = [&](int s, f32x4 (&x)[2][NC], f32x4 (&next)[2][NC]) __attribute__((always_inline)) {
-      // step s + 1 has arrived (step s + 2 may be on its way), and nobody reads step s - 1 any more
-      if (s + 2 < steps)
-        wait_copies<2 * COPIES>();
-      else
-        wait_copies<0>();
-      __syncthreads();
-      if (s + RING - 1 < steps) fetch(s + RING - 1);
       rows.follow(top, p.c);
       uint32_t pairs[NC][4];
       // (behind the last step: the products of whatever lies there, for nobody)
-      products(after(slot), next, [&](auto nc) __attribute__((always_inline)) {
+      products(slot_of(s + 1), next, [&](auto nc) __attribute__((always_inline)) {
         constexpr int n = decltype(nc)::value, each = 16 / (2 * KS);  // of 8 weights, an even number every other group
         if constexpr (each >= 4)
           rows.template weigh_part<each / 2 * n, each / 2 *(n + 1)>(x, p.c, pairs);
@@ -762,10 +742,10 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
       }
       if (s + 1 >= soft) {
         hide(s + 1, next);
-        if (s >= soft) clean_values(s, slot);
+        if (s >= soft) clean_values(s, slot_of(s));
       }
       rows.add_ones(pf);
-      groups_read_ahead<DT>([&](int d) { return v_fragment(slot, d); },
+      groups_read_ahead<DT>([&](int d) { return v_fragment(slot_of(s), d); },
                             [&](auto dc, const bf16x8 &a) __attribute__((always_inline)) {
         constexpr int d = decltype(dc)::value;
 #pragma unroll
@@ -775,21 +755,34 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
           for (int e = 8 / DT * d; e < 8 / DT * (d + 1); ++e) top[c] = e ? fmaxf(top[c], next[e / 4][c][e % 4]) : next[0][c][0];
         }
       });
-      slot = after(slot);
     };
     if (steps > 0) {
+      // (steps behind the last are fetched from page 0 like keys that do not exist)
       load_places(0);
-      for (int s = 0; s < RING - 1 && s < steps; ++s) fetch(s);
+      fetch_k(0);
+      fetch_v(0);
+      fetch_k(1);
+      fetch_v(1);
+      fetch_k(2);
       f32x4 even[2][NC], odd[2][NC];
-      if (steps > 2)
-        wait_copies<2 * 2 * COPIES>();
-      else
-        wait_copies<0>();
+      wait_copies<0>();
       __syncthreads();
       products(0, even, [](auto) {});
       if (0 >= soft) hide(0, even);
       rows.largest(even, top);
       for (int s = 0; s < steps; s += 2) {
+        // K of steps s + 1 and s + 2 and V of steps s and s + 1 have arrived, and nobody reads what came before
+        if (s) {
+          wait_copies<0>();
+          __syncthreads();
+        }
+        if (s + 2 < steps) {
+          if (s + 4 - from_step >= 64) load_places(s + 2);
+          fetch_k(s + 3);
+          fetch_v(s + 2);
+          fetch_k(s + 4);
+          fetch_v(s + 3);
+        }
         step(s, even, odd);
         if (s + 1 < steps) step(s + 1, odd, even);
       }
@@ -806,7 +799,7 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
         for (int d = 0; d < DT; ++d) *(f32x4 *)(p.part_o + at * D + 16 * d + 4 * g) = rows.o[c][d];
         if (g == 0) *(f32x4 *)(p.part_ml + at * 4) = f32x4{rows.m[c], rows.l[c], lr, 0.f};
       } else {
-        const int t = row / p.group, hq = it.kvh * p.group + row - t * p.group;
+        const int t = (int)((uint32_t)row / (uint32_t)p.group), hq = it.kvh * p.group + row - t * p.group;
         const float inv = inverse(lr);
         uint16_t *dst = p.o + (int64_t)(rq.s.first + t) * p.o_st + (int64_t)hq * p.o_sh + 4 * g;
 #pragma unroll
@@ -836,28 +829,33 @@ __global__ __launch_bounds__(CA_THREADS) void cache_join_kernel(CacheAttnParams 
   const int kvh = hq / p.group, row = (token - rq.s.first) * p.group + hq - kvh * p.group;
   const int64_t from = partial_row(rq, kvh, row, 0);
   const int chunks = rq.s.chunks;
-  float top = CA_NONE;
-  for (int c = lane; c < chunks; c += 64) top = fmaxf(top, p.part_ml[(from + c) * 4]);
+  constexpr int AHEAD = 8;
+  // the sums, 64 chunks to a wavefront, and the first results before anything waits for them
+  auto sums = [&](int c) { return c < chunks ? *(const f32x4 *)(p.part_ml + (from + c) * 4) : f32x4{CA_NONE, 0.f, 0.f, 0.f}; };
+  auto results = [&](int c, float (&z)[AHEAD][E]) {
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a)
+#pragma unroll
+      for (int e = 0; e < E; ++e) z[a][e] = p.part_o[(from + min(c + a, chunks - 1)) * D + E * lane + e];
+  };
+  f32x4 ml = sums(lane);
+  float z[AHEAD][E];
+  results(0, z);
+  float top = ml[0];
+  for (int c = lane + 64; c < chunks; c += 64) top = fmaxf(top, sums(c)[0]);
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
   float ls = 0.f, lr = 0.f, y[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) y[e] = 0.f;
   for (int c0 = 0; c0 < chunks; c0 += 64) {
-    const int n = min(64, chunks - c0);
-    f32x4 ml = {CA_NONE, 0.f, 0.f, 0.f};
-    if (lane < n) ml = *(const f32x4 *)(p.part_ml + (from + c0 + lane) * 4);
+    if (c0) ml = sums(c0 + lane);
     const float f = ml[0] == CA_NONE ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
     ls += f * ml[1];
     lr += f * ml[2];
-    const float *src = p.part_o + (from + c0) * D + E * lane;
-    constexpr int AHEAD = 8;
+    const int n = min(64, chunks - c0);
     for (int c = 0; c < n; c += AHEAD) {
-      float z[AHEAD][E];
-#pragma unroll
-      for (int a = 0; a < AHEAD; ++a)
-#pragma unroll
-        for (int e = 0; e < E; ++e) z[a][e] = src[(int64_t)min(c + a, n - 1) * D + e];
+      if (c0 + c) results(c0 + c, z);
 #pragma unroll
       for (int a = 0; a < AHEAD; ++a) {
         const float fc = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), (c + a) & 63));

@@ -37,6 +37,26 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // round to n
 __device__ __forceinline__ bool any_lane(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0ull; }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// inclusive prefix sum over the wavefront by lane moves inside the vector unit (shuffles through LDS take ten times as long)
+template <int CTRL, int ROWS, int BANKS>
+__device__ __forceinline__ uint32_t moved(uint32_t x) {  // zero where the move has no source or the mask leaves the lane out
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, BANKS, false);
+}
+template <int CTRL, int ROWS, int BANKS>
+__device__ __forceinline__ uint64_t moved(uint64_t x) {
+  return moved<CTRL, ROWS, BANKS>((uint32_t)x) | (uint64_t)moved<CTRL, ROWS, BANKS>((uint32_t)(x >> 32)) << 32;
+}
+template <class T>
+__device__ __forceinline__ T wave_prefix(T x) {
+  x += moved<0x111, 0xf, 0xf>(x);  // 1 lane up in the row of 16
+  x += moved<0x112, 0xf, 0xf>(x);  // 2
+  x += moved<0x114, 0xf, 0xe>(x);  // 4
+  x += moved<0x118, 0xf, 0xc>(x);  // 8
+  x += moved<0x142, 0xa, 0xf>(x);  // the row's last lane to the next row
+  x += moved<0x143, 0xc, 0xf>(x);  // the lower half's last lane to the upper half
+  return x;
+}
+
 }  // namespace
 
 #endif

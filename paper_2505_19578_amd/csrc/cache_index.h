@@ -65,24 +65,27 @@ struct CacheShare {
 // Units of a chunk.  It goes by the request's own sizes alone, so that a request's result is the same bits whatever else the
 // call holds: about 16 chunks per 64 rows, so that one request spreads over the chip, of 2 to 8 units per 64 rows, so that a
 // workgroup has enough to do and a long context still makes more workgroups than 16.
-constexpr int64_t cache_chunk_units(int64_t units, int64_t rows) {
-  const int64_t t = (rows + 63) / 64, u = (units * t + 15) / 16;
-  return u < 2 ? 2 : u > 8 * t ? 8 * t : u;
+constexpr uint32_t cache_chunk_units(uint32_t units, uint32_t rows) {
+  const uint32_t t = rows > 64 ? (rows + 63) / 64 : 1, most = 8 * t;
+  if (units >= 128) return most;  // (and 32 bits hold the product below)
+  const uint32_t u = (units * t + 15) / 16;
+  return u < 2 ? 2 : u;
 }
 // Tokens and keys come from device memory: whatever is in it, a share is a share of rows and keys that exist.
-constexpr CacheShare cache_share(int64_t first, int64_t end, int64_t keys, int64_t n_tokens, int64_t most_keys, int group, int tile_rows) {
+constexpr CacheShare cache_share(int32_t first, int32_t end, int32_t keys, int32_t n_tokens, int32_t most_keys, int32_t group,
+                                 int32_t tile_rows) {
   if (first < 0) first = 0;
   if (end > n_tokens) end = n_tokens;
-  const int64_t fresh = end > first ? end - first : 0;
+  const int32_t fresh = end > first ? end - first : 0;
   if (keys > most_keys) keys = most_keys;
   if (keys < fresh) keys = 0;  // a request that the plan refused: no keys, its rows become zeros
   CacheShare s{};
-  s.first = (int32_t)first, s.fresh = (int32_t)fresh, s.keys = (int32_t)keys;
-  s.rows = (int32_t)(fresh * group);
-  s.tiles = (int32_t)((fresh * group + tile_rows - 1) / tile_rows);
-  s.units = keys > 0 ? (int32_t)((keys + CACHE_UNIT - 1) / CACHE_UNIT) : 1;
-  const int64_t u = cache_chunk_units(s.units, s.rows);
-  s.chunks = (int32_t)((s.units + u - 1) / u);
+  s.first = first, s.fresh = fresh, s.keys = keys;
+  s.rows = fresh * group;  // (32 bits hold n_tokens * group)
+  s.tiles = (int32_t)(((uint32_t)s.rows + tile_rows - 1) / (uint32_t)tile_rows);
+  s.units = keys > 0 ? (int32_t)(((uint32_t)keys + CACHE_UNIT - 1) / CACHE_UNIT) : 1;
+  const uint32_t u = cache_chunk_units((uint32_t)s.units, (uint32_t)s.rows);
+  s.chunks = (int32_t)(((uint32_t)s.units + u - 1) / u);
   return s;
 }
 // Upper bounds of what all requests of a call add up to, per KV head; the kernels' sums never pass them.
@@ -111,13 +114,11 @@ constexpr int64_t cache_grid(int64_t n_requests, int64_t n_tokens, int group, in
 struct CachePlace {
   int32_t pair, tile;
 };
-constexpr CachePlace cache_place(int32_t index, int32_t pairs, int32_t tiles) {
-  const int32_t eight = index / (8 * tiles), rest = index - eight * 8 * tiles;
-  const int32_t wide = pairs - 8 * eight < 8 ? pairs - 8 * eight : 8;
-  return CachePlace{8 * eight + rest % wide, rest / wide};
-}
-constexpr int32_t cache_index_of(int32_t pair, int32_t tile, int32_t pairs, int32_t tiles) {
-  const int32_t eight = pair / 8, wide = pairs - 8 * eight < 8 ? pairs - 8 * eight : 8;
-  return eight * 8 * tiles + tile * wide + pair % 8;
+constexpr CachePlace cache_place(uint32_t index, uint32_t pairs, uint32_t tiles) {
+  if (tiles == 1) return CachePlace{(int32_t)index, 0};
+  const uint32_t eight = index / (8 * tiles), rest = index - eight * 8 * tiles;
+  const uint32_t wide = pairs - 8 * eight < 8 ? pairs - 8 * eight : 8;
+  if (wide == 8) return CachePlace{(int32_t)(8 * eight + rest % 8), (int32_t)(rest / 8)};
+  return CachePlace{(int32_t)(8 * eight + rest % wide), (int32_t)(rest / wide)};
 }
 #endif
