@@ -162,7 +162,7 @@ sp_status launch_cache_attn(const CacheAttnParams &p, int tile_rows, int64_t ite
   const sp_status rc = launched("cache_attn_kernel");
   if (rc || cache_most_chunks(p.most_keys) == 1) return rc;  // no request has two chunks
   const int64_t rows = (int64_t)p.n_tok * p.hq;
-  hipLaunchKernelGGL((cache_join_kernel<D>), dim3((unsigned)((rows + CA_WAVES - 1) / CA_WAVES)), block, 0, st, p);
+  hipLaunchKernelGGL((cache_join_kernel<D>), dim3((unsigned)std::min((rows + CA_WAVES - 1) / CA_WAVES, CA_GRID)), block, 0, st, p);
   return launched("cache_join_kernel");
 }
 
@@ -220,7 +220,7 @@ sp_status sp_cache_plan(int32_t n_requests, int32_t max_tokens, int32_t page_siz
   const bool one = max_tokens <= PLAN_ONE_LAUNCH;
   hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, p, one ? 1 : 0);
   if ((rc = launched("plan_kernel")) || one) return rc;
-  hipLaunchKernelGGL(plan_tokens_kernel, dim3((unsigned)((max_tokens + PLAN_PART_TOKENS - 1) / PLAN_PART_TOKENS)), dim3(PLAN_PART_THREADS),
+  hipLaunchKernelGGL(plan_tokens_kernel, dim3((unsigned)((max_tokens + PLAN_PART_THREADS - 1) / PLAN_PART_THREADS)), dim3(PLAN_PART_THREADS),
                      0, st, p);
   return launched("plan_tokens_kernel");
 }

@@ -51,18 +51,21 @@ struct CacheRequest {
   int r;
   int items_before;  // workgroups' items of the requests before it
   int rows_before;   // rows of partial results of the requests before it
+  int joins_before;  // rows to join of the requests before it
 };
 
-// Walks the requests of a call forward, 64 at a time, one to a lane.
+// Walks the requests of a call forward, 64 at a time, one to a lane.  (Made anew for each item: kept, it would take registers from the
+// loops.)
 template <int TILE>
 struct CacheWalk {
   const CacheAttnParams &p;
   const int lane;
-  int r0 = 0, items = 0, rows = 0;  // requests, items and rows of partial results before the present 64
+  // requests, items, rows of partial results and rows to join (of chunked requests, all KV heads) before the present 64
+  int r0 = 0, items = 0, rows = 0, joins = 0;
   int first, end, keys;  // of this lane's request, as the arrays hold them
-  int upto, parts;       // items and rows up to and with it
+  int upto, parts, joint;  // items, rows and rows to join up to and with it
   bool good;
-  __device__ __forceinline__ CacheWalk(const CacheAttnParams &params, int l) : p(params), lane(l) { look(); }
+  __device__ __forceinline__ CacheWalk(const CacheAttnParams &params, int l) : p(reloaded(params)), lane(l) { look(); }
   __device__ __forceinline__ void look() {
     const int r = r0 + lane;
     const bool live = r < p.n_req;
@@ -71,6 +74,7 @@ struct CacheWalk {
     good = !any_lane(end < first);  // otherwise this is no tok_start: nothing behind is done, so that no index leaves its buffer
     upto = items + (int)wave_prefix((uint32_t)(s.tiles * p.hk * s.chunks));
     parts = rows + (int)wave_prefix((uint32_t)(s.chunks > 1 ? s.rows * p.hk * s.chunks : 0));
+    joint = joins + (int)wave_prefix((uint32_t)(s.chunks > 1 ? s.rows * p.hk : 0));
   }
   template <class Test>
   __device__ __forceinline__ bool seek(Test &&test, CacheRequest &out) {
@@ -84,11 +88,13 @@ struct CacheWalk {
         out.r = r0 + at;
         out.items_before = of(upto) - out.s.tiles * p.hk * out.s.chunks;
         out.rows_before = of(parts) - (out.s.chunks > 1 ? out.s.rows * p.hk * out.s.chunks : 0);
+        out.joins_before = of(joint) - (out.s.chunks > 1 ? out.s.rows * p.hk : 0);
         return true;
       }
       if (r0 + 64 >= p.n_req) return false;
       items = __builtin_amdgcn_readlane(upto, 63);
       rows = __builtin_amdgcn_readlane(parts, 63);
+      joins = __builtin_amdgcn_readlane(joint, 63);
       r0 += 64;
       look();
     }
@@ -96,8 +102,8 @@ struct CacheWalk {
   __device__ __forceinline__ bool item(int index, CacheRequest &out) {
     return seek([index](const CacheWalk &w) { return w.upto > index; }, out);
   }
-  __device__ __forceinline__ bool token(int t, CacheRequest &out) {
-    return seek([t](const CacheWalk &w) { return w.end > w.first && w.end > t; }, out);
+  __device__ __forceinline__ bool join(int index, CacheRequest &out) {
+    return seek([index](const CacheWalk &w) { return w.joint > index; }, out);
   }
 };
 
@@ -161,6 +167,7 @@ struct CacheRows {
   f32x4 o[NC][DT], ones[NC];
   // reference (log2), what a product has to exceed to move it, sum of the weights
   float m[NC], limit[NC], l[NC];
+  int tok[NC];  // the column's new token
 
   __device__ __forceinline__ void begin(const CacheAttnParams &p, const CacheRequest &rq, int kvh, int row0, int g, int i) {
 #pragma unroll
@@ -168,6 +175,7 @@ struct CacheRows {
       const int row = row0 + 16 * c + i;
       const bool live = row < rq.s.rows;
       const int t = live ? (int)((uint32_t)row / (uint32_t)p.group) : 0, hq = kvh * p.group + (live ? row - t * p.group : 0);
+      tok[c] = t;
       const uint16_t *src = p.q + (int64_t)(rq.s.first + t) * p.q_st + (int64_t)hq * p.q_sh + 8 * g;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -175,6 +183,11 @@ struct CacheRows {
         if (!live) x = u32x4{0, 0, 0, 0};
         q[c][s] = __builtin_bit_cast(bf16x8, x);
       }
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[c][d] = f32x4{0.f, 0.f, 0.f, 0.f};
       ones[c] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -183,12 +196,14 @@ struct CacheRows {
       l[c] = 0.f;
     }
   }
-  // bits of the step's keys that a row sees, from key 4 g of each half on (bits 0 .. 3 and 16 .. 19)
-  static __device__ __forceinline__ uint32_t sees(const CacheAttnParams &p, const CacheRequest &rq, const CacheItem &it, int row,
-                                                  int kb, uint32_t there, int g) {
-    const int t = row < rq.s.rows ? (int)((uint32_t)row / (uint32_t)p.group) : 0;
-    const uint64_t *mask = p.words ? p.mask + (int64_t)(rq.s.first + t) * p.words : nullptr;
-    return (cache_visible(kb, it.ctx, rq.s.fresh, t, mask, p.words) & there) >> (4 * g);
+  // Bits of the step's keys that column c's query sees, from key 4 g of each half on (bits 0 .. 3 and 16 .. 19).  mask: the words of
+  // its token, if there are any.
+  __device__ __forceinline__ uint32_t sees(const CacheRequest &rq, const CacheItem &it, int c, int kb, uint32_t there, int g, int words,
+                                           const uint64_t *mask) const {
+    const uint32_t see = words == 0   ? cache_visible_chain(kb, it.ctx, rq.s.fresh, tok[c])
+                         : words == 1 ? cache_visible_word(kb, it.ctx, rq.s.fresh, mask[0])
+                                      : cache_visible_words(kb, it.ctx, rq.s.fresh, mask, words);
+    return (see & there) >> (4 * g);
   }
   // A step's products x (keys that are not seen: -infinity) in three parts: the largest of each column's, ..
   __device__ __forceinline__ void largest(const f32x4 (&x)[2][NC], float (&top)[NC]) const {
@@ -283,6 +298,16 @@ struct CacheRows {
       }
     }
   }
+  __device__ __forceinline__ bool any_odd() const {
+    uint32_t high = 0;  // an exponent of ones stays the largest
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) high = max(high, __builtin_bit_cast(uint32_t, o[c][d][r]) & 0x7fffffffu);
+    return any_lane(high >= 0x7f800000u);
+  }
   // row sums over the lanes that share a column
   __device__ __forceinline__ void finish() {
 #pragma unroll
@@ -329,13 +354,12 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_narrow_kernel(CacheA
   const uint32_t k_lane = 2u * (uint32_t)(i * (int)p.c_st + 8 * g);  // bytes
   const uint32_t v_lane = 2u * (uint32_t)((lane / VL) * (int)p.c_st + 8 * (lane % VL));
 
-  CacheWalk<ROWS> walk(p, lane);
   CacheRequest rq;
-  for (int index = blockIdx.x; walk.item(index, rq); index += gridDim.x) {
-    const CacheItem it = item_of(rq, index, p.hk);
+  for (int index = blockIdx.x; CacheWalk<ROWS>(p, lane).item(index, rq); index += gridDim.x) {
+    const CacheItem it = item_of(rq, index, reloaded(p).hk);
     CacheRows<D, NC> rows;
     const int row0 = it.tile * ROWS;
-    rows.begin(p, rq, it.kvh, row0, g, i);
+    rows.begin(reloaded(p), rq, it.kvh, row0, g, i);
 
     // Pages of 32 of the wavefront's steps at a time: lane 2 s + half holds that of step s, keys 16 half .. 16 half + 15 (a page
     // holds 16 keys and more, and begins at a multiple of them); -1: no such key, or a page that the cache does not have.
@@ -382,90 +406,94 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_narrow_kernel(CacheA
       id1 = __builtin_amdgcn_readlane(pages, 2 * (s - pages_from) + 1);
     };
 
-    if (steps > 0) {
-      load_pages(0);
-      take_ids(0);
-      load_k(step_key(0), id0, id1);
-      load_v(step_key(0), id0, id1);
-    }
-    for (int s = 0; s < steps; ++s) {
-      const int kb = step_key(s), was0 = id0, was1 = id1;
-      f32x4 x[2][NC];
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int y = 0; y < KS; ++y)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[j][y]), rows.q[c][y], acc, 0, 0, 0);
-          x[j][c] = acc;
-        }
-      if (s + 1 < steps) {
-        take_ids(s + 1);
-        load_k(step_key(s + 1), id0, id1);
+    // A second time, with care, if anything of O is not finite: a product of weight zero with an infinite value is NaN.  With care
+    // values that are not finite are kept out of the products and added to the rows that see them.
+    for (bool careful = false;; careful = true) {
+      rows.clear();
+      if (steps > 0) {
+        load_pages(0);
+        take_ids(0);
+        load_k(step_key(0), id0, id1);
+        load_v(step_key(0), id0, id1);
       }
-      // all keys of a step in the context are seen by every row
-      const bool whole = kb + CACHE_STEP <= it.ctx && was0 >= 0 && was1 >= 0;
-      const uint32_t there = (was0 < 0 ? 0u : 0xffffu) | (was1 < 0 ? 0u : 0xffff0000u);
-      auto no_value = [&](int n) { return kb + (64 / VL) * n + lane / VL >= it.k_end || (n < NV / 2 ? was0 : was1) < 0; };
-      bool odd_values = false;
-      if (!whole) {
+      for (int s = 0; s < steps; ++s) {
+        const int kb = step_key(s), was0 = id0, was1 = id1;
+        f32x4 x[2][NC];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const uint32_t see = rows.sees(p, rq, it, row0 + 16 * c + i, kb, there, g);
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int c = 0; c < NC; ++c) {
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (!((see >> (16 * j + r)) & 1)) x[j][c][r] = -INFINITY;
+            for (int y = 0; y < KS; ++y)
+              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[j][y]), rows.q[c][y], acc, 0, 0, 0);
+            x[j][c] = acc;
+          }
+        if (s + 1 < steps) {
+          take_ids(s + 1);
+          load_k(step_key(s + 1), id0, id1);
         }
-        // values of keys that do not exist count as zeros; values that are not finite are kept out of the product and added to
-        // the rows that see them (below)
-        bool odd = false;
+        // all keys of a step in the context are seen by every row
+        const bool exist = was0 >= 0 && was1 >= 0;
+        const uint32_t there = (was0 < 0 ? 0u : 0xffffu) | (was1 < 0 ? 0u : 0xffff0000u);
+        auto no_value = [&](int n) { return kb + (64 / VL) * n + lane / VL >= it.k_end || (n < NV / 2 ? was0 : was1) < 0; };
+        const CacheAttnParams &cp = reloaded(p);
+        auto mask_of = [&](int c) { return cp.mask + (int64_t)(rq.s.first + rows.tok[c]) * cp.words; };
+        if (kb + CACHE_STEP > it.ctx || !exist) {
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-          if (no_value(n)) vr[n] = u32x4{0, 0, 0, 0};
+          for (int c = 0; c < NC; ++c) {
+            const uint32_t see = rows.sees(rq, it, c, kb, there, g, cp.words, mask_of(c));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            odd |= odd_bf16x2(vr[n][e]);
-            vr[n][e] = without_odd(vr[n][e]);
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (!((see >> (16 * j + r)) & 1)) x[j][c][r] = -INFINITY;
           }
         }
-        odd_values = any_lane(odd);
-      }
-      store_v(vr);
-      float top[NC];
-      rows.largest(x, top);
-      rows.follow(top, p.c);
-      uint32_t pairs[NC][4];
-      rows.template weigh_part<0, 8>(x, p.c, pairs);
-      bf16x8 pf[NC];
+        if (kb + CACHE_STEP > it.k_end || !exist)  // values of keys that do not exist count as zeros
 #pragma unroll
-      for (int c = 0; c < NC; ++c) pf[c] = rows.weights_of(pairs[c]);
-      rows.add_ones(pf);
-      if (!odd_values && s + 1 < steps) load_v(step_key(s + 1), id0, id1);
-      rows.add_values(pf, v_fragment);
-      if (odd_values) {
-        bf16x8 seen[NC];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) seen[c] = rows.as_ones(rows.sees(p, rq, it, row0 + 16 * c + i, kb, there, g));
-#pragma unroll 1
-        for (int kind = 0; kind < ODD_KINDS; ++kind) {
-          load_v(kb, was0, was1);
+          for (int n = 0; n < NV; ++n)
+            if (no_value(n)) vr[n] = u32x4{0, 0, 0, 0};
+        if (careful)
 #pragma unroll
           for (int n = 0; n < NV; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) vr[n][e] = no_value(n) ? 0u : ones_of_kind(vr[n][e], kind);
-          store_v(vr);
-          rows.add_kind(seen, kind, v_fragment);
+            for (int e = 0; e < 4; ++e) vr[n][e] = without_odd(vr[n][e]);
+        store_v(vr);
+        if (!careful && s + 1 < steps) load_v(step_key(s + 1), id0, id1);
+        float top[NC];
+        rows.largest(x, top);
+        rows.follow(top, p.c);
+        uint32_t pairs[NC][4];
+        rows.template weigh_part<0, 8>(x, p.c, pairs);
+        bf16x8 pf[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) pf[c] = rows.weights_of(pairs[c]);
+        rows.add_ones(pf);
+        rows.add_values(pf, v_fragment);
+        if (careful) {
+          bf16x8 seen[NC];
+#pragma unroll
+          for (int c = 0; c < NC; ++c) seen[c] = rows.as_ones(rows.sees(rq, it, c, kb, there, g, cp.words, mask_of(c)));
+#pragma unroll 1
+          for (int kind = 0; kind < ODD_KINDS; ++kind) {
+            load_v(kb, was0, was1);
+#pragma unroll
+            for (int n = 0; n < NV; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) vr[n][e] = no_value(n) ? 0u : ones_of_kind(vr[n][e], kind);
+            store_v(vr);
+            rows.add_kind(seen, kind, v_fragment);
+          }
+          if (s + 1 < steps) load_v(step_key(s + 1), id0, id1);
         }
-        if (s + 1 < steps) load_v(step_key(s + 1), id0, id1);
       }
+      if (careful || !rows.any_odd()) break;
     }
 
     // the four wavefronts add up, sixteen rows at a time
     rows.finish();
+    const CacheAttnParams &q = reloaded(p);
     __syncthreads();  // (the last item's sums are read)
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -514,16 +542,16 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_narrow_kernel(CacheA
       if (rq.s.chunks > 1) {
         const int64_t at = partial_row(rq, it.kvh, row, it.chunk);
 #pragma unroll
-        for (int e = 0; e < E; e += 4) *(f32x4 *)(p.part_o + at * D + E * piece + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
-        if (piece == 0) *(f32x4 *)(p.part_ml + at * 4) = f32x4{top, ls, lr, 0.f};
+        for (int e = 0; e < E; e += 4) *(f32x4 *)(q.part_o + at * D + E * piece + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
+        if (piece == 0) *(f32x4 *)(q.part_ml + at * 4) = f32x4{top, ls, lr, 0.f};
       } else {
-        const int t = (int)((uint32_t)row / (uint32_t)p.group), hq = it.kvh * p.group + row - t * p.group;
+        const int t = (int)((uint32_t)row / (uint32_t)q.group), hq = it.kvh * q.group + row - t * q.group;
         const float inv = inverse(lr);
-        uint16_t *dst = p.o + (int64_t)(rq.s.first + t) * p.o_st + (int64_t)hq * p.o_sh + E * piece;
+        uint16_t *dst = q.o + (int64_t)(rq.s.first + t) * q.o_st + (int64_t)hq * q.o_sh + E * piece;
 #pragma unroll
         for (int e = 0; e < E; e += 4)
           *(u32x2 *)(dst + e) = u32x2{pack_bf16(y[e] * inv, y[e + 1] * inv), pack_bf16(y[e + 2] * inv, y[e + 3] * inv)};
-        if (p.lse && piece == 0) p.lse[(int64_t)(rq.s.first + t) * p.hq + hq] = lse_of(top, ls);
+        if (q.lse && piece == 0) q.lse[(int64_t)(rq.s.first + t) * q.hq + hq] = lse_of(top, ls);
       }
     }
     __syncthreads();  // the sums lie where V of the next item will
@@ -587,6 +615,7 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
   constexpr int COPY_ROWS = 1024 / ROWB;        // rows that one copy moves
   constexpr int COPIES = CACHE_STEP / CA_WAVES / COPY_ROWS;  // copies of a wavefront for its 8 rows of K (and as many for V)
   __shared__ __attribute__((aligned(1024))) char smem[RING * 2 * TILE];  // slot n: K of a step, then V of a step
+  __shared__ uint64_t words[ROWS * CACHE_MAX_WORDS];  // mask words of the tile's rows
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) char *)smem;
 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, i = lane & 15;
@@ -616,16 +645,23 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
   };
   auto slot_of = [](int s) { return (uint32_t)(s % RING) * (2 * TILE); };
 
-  CacheWalk<ROWS> walk(p, lane);
   CacheRequest rq;
-  for (int index = blockIdx.x; walk.item(index, rq); index += gridDim.x) {
-    const CacheItem it = item_of(rq, index, p.hk);
+  for (int index = blockIdx.x; CacheWalk<ROWS>(p, lane).item(index, rq); index += gridDim.x) {
+    const CacheItem it = item_of(rq, index, reloaded(p).hk);
     CacheRows<D, NC> rows;
     const int row0 = it.tile * ROWS + w * WROWS;
-    rows.begin(p, rq, it.kvh, row0, g, i);
+    const bool idle = row0 >= rq.s.rows;  // no rows are left for this wavefront
+    rows.begin(reloaded(p), rq, it.kvh, row0, g, i);
+    if (const CacheAttnParams &cp = reloaded(p); cp.words)  // (the ring's first barrier lies before their use)
+      for (int n = tid; n < ROWS * cp.words; n += CA_THREADS) {
+        const int r = (int)((uint32_t)n / (uint32_t)cp.words), row = it.tile * ROWS + r;
+        if (row < rq.s.rows)
+          words[n] = cp.mask[(int64_t)(rq.s.first + (int)((uint32_t)row / (uint32_t)cp.group)) * cp.words + (n - r * cp.words)];
+      }
     const int steps = it.k_begin < it.k_end ? (it.k_end - it.k_begin + CACHE_STEP - 1) / CACHE_STEP : 0;
-    // All keys of a step before `soft` lie in the context and on pages that exist: every row sees them.
-    int soft = it.ctx > it.k_begin ? (it.ctx - it.k_begin) / CACHE_STEP : 0;
+    // All keys of a step before `soft` lie in the context and on pages that exist: every row sees them.  All keys of a step before
+    // `holes` exist.
+    int soft = it.ctx > it.k_begin ? (it.ctx - it.k_begin) / CACHE_STEP : 0, holes = (it.k_end - it.k_begin) / CACHE_STEP;
     auto page_at = [&](const CacheAttnParams &c, int key) {
       if (key >= it.k_end) return -1;
       const int id = c.table[(int64_t)rq.r * c.width + (key >> c.page_shift)];
@@ -640,7 +676,11 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
       const int key = it.k_begin + CACHE_STEP * (s0 + lane), mine = key + 16 * (w >> 1);
       const int a = page_at(c, key), b = page_at(c, key + 16), id = w >> 1 ? b : a;
       const uint64_t none = __builtin_amdgcn_ballot_w64(key < it.k_end && (a < 0 || (b < 0 && key + 16 < it.k_end)));
-      if (none) soft = min(soft, s0 + (int)__builtin_ctzll(none));
+      if (none) {
+        const int first = s0 + (int)__builtin_ctzll(none);
+        soft = min(soft, first);
+        holes = min(holes, first);
+      }
       const uint64_t at = 2 * ((uint64_t)(id < 0 ? 0 : id) * (uint64_t)c.c_sp +
                                (uint64_t)(mine & ((1 << c.page_shift) - 1)) * (uint64_t)c.c_st + (uint64_t)it.kvh * (uint64_t)c.c_sh);
       from_low = (uint32_t)at, from_high = (uint32_t)(at >> 32);
@@ -674,7 +714,7 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
       const uint32_t exist = there(cp, kb);
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const uint32_t see = rows.sees(cp, rq, it, row0 + 16 * c + i, kb, exist, g);
+        const uint32_t see = rows.sees(rq, it, c, kb, exist, g, cp.words, words + (w * WROWS + 16 * c + i) * cp.words);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -682,45 +722,18 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
             if (!((see >> (16 * j + r)) & 1)) x[j][c][r] = -INFINITY;
       }
     };
-    // Values of such a step: those of keys that do not exist become zeros; those that are not finite are kept out of the product
-    // and added here to the rows that see them.
-    auto clean_values = [&](int s, uint32_t slot) __attribute__((always_inline)) {
-      constexpr int OWN = TILE / 16 / CA_THREADS;  // pieces of V that are this thread's to look at
-      const CacheAttnParams &cp = reloaded(p);
-      char *const vt = smem + slot + TILE;
-      const int kb = it.k_begin + CACHE_STEP * s;
-      const uint32_t exist = there(cp, kb);
-      int odd = 0;
+    constexpr int OWN = TILE / 16 / CA_THREADS;  // pieces of a step's V that are this thread's to look at
+    auto own_piece = [&](int s, int n) { return smem + slot_of(s) + TILE + (n * CA_THREADS + tid) * 16; };
+    auto exists = [&](int s, int n, uint32_t exist) {  // the key of such a piece
+      const int r = (n * CA_THREADS + tid) * 16 / ROWB;
+      return it.k_begin + CACHE_STEP * s + r < it.k_end && ((exist >> r) & 1);
+    };
+    // values of keys that do not exist become zeros
+    auto clear_holes = [&](int s) {
+      const uint32_t exist = there(reloaded(p), it.k_begin + CACHE_STEP * s);
 #pragma unroll
-      for (int n = 0; n < OWN; ++n) {
-        const int at = (n * CA_THREADS + tid) * 16, r = at / ROWB;
-        const u32x4 y = *(const u32x4 *)(vt + at);
-        if (kb + r >= it.k_end || !((exist >> r) & 1))
-          *(u32x4 *)(vt + at) = u32x4{0, 0, 0, 0};
-        else
-          odd |= odd_bf16x2(y[0]) || odd_bf16x2(y[1]) || odd_bf16x2(y[2]) || odd_bf16x2(y[3]);
-      }
-      if (!__syncthreads_or(odd)) return;
-      bf16x8 seen[NC];
-#pragma unroll
-      for (int c = 0; c < NC; ++c) seen[c] = rows.as_ones(rows.sees(cp, rq, it, row0 + 16 * c + i, kb, exist, g));
-      u32x4 keep[OWN];
-#pragma unroll
-      for (int n = 0; n < OWN; ++n) keep[n] = *(const u32x4 *)(vt + (n * CA_THREADS + tid) * 16);
-#pragma unroll 1
-      for (int kind = 0; kind <= ODD_KINDS; ++kind) {  // the last round leaves the finite values
-#pragma unroll
-        for (int n = 0; n < OWN; ++n) {
-          u32x4 y;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = kind == ODD_KINDS ? without_odd(keep[n][e]) : ones_of_kind(keep[n][e], kind);
-          *(u32x4 *)(vt + (n * CA_THREADS + tid) * 16) = y;
-        }
-        __syncthreads();
-        if (kind == ODD_KINDS) break;
-        rows.add_kind(seen, kind, [&](int d) { return v_fragment(slot, d); });
-        __syncthreads();
-      }
+      for (int n = 0; n < OWN; ++n)
+        if (!exists(s, n, exist)) *(u32x4 *)own_piece(s, n) = u32x4{0, 0, 0, 0};
     };
     float top[NC];
     auto step = [&](int s, f32x4 (&x)[2][NC], f32x4 (&next)[2][NC]) __attribute__((always_inline)) {
@@ -740,10 +753,7 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
         asm volatile("" : "+v"(pairs[c][0]), "+v"(pairs[c][1]), "+v"(pairs[c][2]), "+v"(pairs[c][3]));  // made here, not where they are used
         pf[c] = rows.weights_of(pairs[c]);
       }
-      if (s + 1 >= soft) {
-        hide(s + 1, next);
-        if (s >= soft) clean_values(s, slot_of(s));
-      }
+      if (s + 1 >= soft) hide(s + 1, next);
       rows.add_ones(pf);
       groups_read_ahead<DT>([&](int d) { return v_fragment(slot_of(s), d); },
                             [&](auto dc, const bf16x8 &a) __attribute__((always_inline)) {
@@ -756,6 +766,7 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
         }
       });
     };
+    rows.clear();
     if (steps > 0) {
       // (steps behind the last are fetched from page 0 like keys that do not exist)
       load_places(0);
@@ -767,9 +778,11 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
       f32x4 even[2][NC], odd[2][NC];
       wait_copies<0>();
       __syncthreads();
-      products(0, even, [](auto) {});
-      if (0 >= soft) hide(0, even);
-      rows.largest(even, top);
+      if (!idle) {
+        products(0, even, [](auto) {});
+        if (0 >= soft) hide(0, even);
+        rows.largest(even, top);
+      }
       for (int s = 0; s < steps; s += 2) {
         // K of steps s + 1 and s + 2 and V of steps s and s + 1 have arrived, and nobody reads what came before
         if (s) {
@@ -783,11 +796,69 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
           fetch_k(s + 4);
           fetch_v(s + 3);
         }
-        step(s, even, odd);
-        if (s + 1 < steps) step(s + 1, odd, even);
+        if (s + 1 >= holes) {
+          clear_holes(s);
+          clear_holes(s + 1);
+          __syncthreads();
+        }
+        if (!idle) {
+          step(s, even, odd);
+          if (s + 1 < steps) step(s + 1, odd, even);
+        }
+      }
+    }
+    // (with this barrier nobody reads the ring any more)
+    if (__syncthreads_or(rows.any_odd())) {
+      // Something of O is not finite, and a product of weight zero with an infinite value is NaN: once more, step by step, with
+      // the values that are not finite kept out of the product and added to the rows that see them.
+      rows.clear();
+#pragma unroll 1
+      for (int s = 0; s < steps; ++s) {
+        if (s == 0 || s - from_step >= 64 || s < from_step) load_places(s);
+        fetch_k(s);
+        fetch_v(s);
+        wait_copies<0>();
+        __syncthreads();
+        f32x4 x[2][NC];
+        products(slot_of(s), x, [](auto) {});
+        hide(s, x);
+        rows.largest(x, top);
+        rows.follow(top, p.c);
+        uint32_t pairs[NC][4];
+        rows.template weigh_part<0, 8>(x, p.c, pairs);
+        bf16x8 pf[NC], seen[NC];
+        const int kb = it.k_begin + CACHE_STEP * s;
+        const CacheAttnParams &cp = reloaded(p);
+        const uint32_t exist = there(cp, kb);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          pf[c] = rows.weights_of(pairs[c]);
+          seen[c] = rows.as_ones(rows.sees(rq, it, c, kb, exist, g, cp.words, words + (w * WROWS + 16 * c + i) * cp.words));
+        }
+        rows.add_ones(pf);
+        u32x4 keep[OWN];
+#pragma unroll
+        for (int n = 0; n < OWN; ++n) keep[n] = exists(s, n, exist) ? *(const u32x4 *)own_piece(s, n) : u32x4{0, 0, 0, 0};
+#pragma unroll 1
+        for (int kind = 0; kind <= ODD_KINDS; ++kind) {  // the last round is of the finite values
+#pragma unroll
+          for (int n = 0; n < OWN; ++n) {
+            u32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = kind == ODD_KINDS ? without_odd(keep[n][e]) : ones_of_kind(keep[n][e], kind);
+            *(u32x4 *)own_piece(s, n) = y;
+          }
+          __syncthreads();
+          if (kind < ODD_KINDS)
+            rows.add_kind(seen, kind, [&](int d) { return v_fragment(slot_of(s), d); });
+          else
+            rows.add_values(pf, [&](int d) { return v_fragment(slot_of(s), d); });
+          __syncthreads();
+        }
       }
     }
     rows.finish();
+    const CacheAttnParams &e = reloaded(p);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int row = row0 + 16 * c + i;
@@ -796,87 +867,86 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
       if (rq.s.chunks > 1) {
         const int64_t at = partial_row(rq, it.kvh, row, it.chunk);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *(f32x4 *)(p.part_o + at * D + 16 * d + 4 * g) = rows.o[c][d];
-        if (g == 0) *(f32x4 *)(p.part_ml + at * 4) = f32x4{rows.m[c], rows.l[c], lr, 0.f};
+        for (int d = 0; d < DT; ++d) *(f32x4 *)(e.part_o + at * D + 16 * d + 4 * g) = rows.o[c][d];
+        if (g == 0) *(f32x4 *)(e.part_ml + at * 4) = f32x4{rows.m[c], rows.l[c], lr, 0.f};
       } else {
-        const int t = (int)((uint32_t)row / (uint32_t)p.group), hq = it.kvh * p.group + row - t * p.group;
+        const int t = (int)((uint32_t)row / (uint32_t)e.group), hq = it.kvh * e.group + row - t * e.group;
         const float inv = inverse(lr);
-        uint16_t *dst = p.o + (int64_t)(rq.s.first + t) * p.o_st + (int64_t)hq * p.o_sh + 4 * g;
+        uint16_t *dst = e.o + (int64_t)(rq.s.first + t) * e.o_st + (int64_t)hq * e.o_sh + 4 * g;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           const f32x4 y = rows.o[c][d] * inv;
           *(u32x2 *)(dst + 16 * d) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
         }
-        if (p.lse && g == 0) p.lse[(int64_t)(rq.s.first + t) * p.hq + hq] = lse_of(rows.m[c], rows.l[c]);
+        if (e.lse && g == 0) e.lse[(int64_t)(rq.s.first + t) * e.hq + hq] = lse_of(rows.m[c], rows.l[c]);
       }
     }
-    __syncthreads();  // the ring is read: the next item's steps may be fetched
   }
 }
 
 // ------------------------------------------------------------------------------------------------------------------ join
-// Joins the chunks of a row, in their order: a wavefront per row.
+// Joins the chunks of the rows that have several, in their order: a wavefront per row, and on to the row as many wavefronts as the
+// launch has further on.
 template <int D>
 __global__ __launch_bounds__(CA_THREADS) void cache_join_kernel(CacheAttnParams p) {
   constexpr int E = D / 64;
   const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * CA_WAVES + uniform(threadIdx.x >> 6);
-  const int token = (int)(at / p.hq), hq = (int)(at - (int64_t)token * p.hq);
-  if (token >= p.n_tok) return;
-  CacheWalk<16> walk(p, lane);  // (nothing here depends on the tiles)
+  CacheWalk<16> walk(p, lane);  // (nothing here depends on the tiles; rows are short work: it is kept)
   CacheRequest rq;
-  if (!walk.token(token, rq) || rq.s.chunks == 1 || token < rq.s.first) return;
-  const int kvh = hq / p.group, row = (token - rq.s.first) * p.group + hq - kvh * p.group;
-  const int64_t from = partial_row(rq, kvh, row, 0);
-  const int chunks = rq.s.chunks;
-  constexpr int AHEAD = 8;
-  // the sums, 64 chunks to a wavefront, and the first results before anything waits for them
-  auto sums = [&](int c) { return c < chunks ? *(const f32x4 *)(p.part_ml + (from + c) * 4) : f32x4{CA_NONE, 0.f, 0.f, 0.f}; };
-  auto results = [&](int c, float (&z)[AHEAD][E]) {
+  for (int index = (int)blockIdx.x * CA_WAVES + uniform(threadIdx.x >> 6); walk.join(index, rq); index += (int)gridDim.x * CA_WAVES) {
+    const int in = index - rq.joins_before, kvh = (int)((uint32_t)in / (uint32_t)rq.s.rows), row = in - kvh * rq.s.rows;
+    const int t = (int)((uint32_t)row / (uint32_t)p.group), token = rq.s.first + t, hq = kvh * p.group + row - t * p.group;
+    const int64_t from = partial_row(rq, kvh, row, 0);
+    const int chunks = rq.s.chunks;
+    constexpr int AHEAD = 8;
+    // the sums, 64 chunks to a wavefront, and the first results before anything waits for them
+    auto sums = [&](int c) { return c < chunks ? *(const f32x4 *)(p.part_ml + (from + c) * 4) : f32x4{CA_NONE, 0.f, 0.f, 0.f}; };
+    auto results = [&](int c, float (&z)[AHEAD][E]) {
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a)
+      for (int a = 0; a < AHEAD; ++a)
 #pragma unroll
-      for (int e = 0; e < E; ++e) z[a][e] = p.part_o[(from + min(c + a, chunks - 1)) * D + E * lane + e];
-  };
-  f32x4 ml = sums(lane);
-  float z[AHEAD][E];
-  results(0, z);
-  float top = ml[0];
-  for (int c = lane + 64; c < chunks; c += 64) top = fmaxf(top, sums(c)[0]);
+        for (int e = 0; e < E; ++e) z[a][e] = p.part_o[(from + min(c + a, chunks - 1)) * D + E * lane + e];
+    };
+    f32x4 ml = sums(lane);
+    float z[AHEAD][E];
+    results(0, z);
+    float top = ml[0];
+    for (int c = lane + 64; c < chunks; c += 64) top = fmaxf(top, sums(c)[0]);
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  float ls = 0.f, lr = 0.f, y[E];
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    float ls = 0.f, lr = 0.f, y[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) y[e] = 0.f;
-  for (int c0 = 0; c0 < chunks; c0 += 64) {
-    if (c0) ml = sums(c0 + lane);
-    const float f = ml[0] == CA_NONE ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
-    ls += f * ml[1];
-    lr += f * ml[2];
-    const int n = min(64, chunks - c0);
-    for (int c = 0; c < n; c += AHEAD) {
-      if (c0 + c) results(c0 + c, z);
+    for (int e = 0; e < E; ++e) y[e] = 0.f;
+    for (int c0 = 0; c0 < chunks; c0 += 64) {
+      if (c0) ml = sums(c0 + lane);
+      const float f = ml[0] == CA_NONE ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
+      ls += f * ml[1];
+      lr += f * ml[2];
+      const int n = min(64, chunks - c0);
+      for (int c = 0; c < n; c += AHEAD) {
+        if (c0 + c) results(c0 + c, z);
 #pragma unroll
-      for (int a = 0; a < AHEAD; ++a) {
-        const float fc = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), (c + a) & 63));
-        if (c + a < n && fc != 0.f)
+        for (int a = 0; a < AHEAD; ++a) {
+          const float fc = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), (c + a) & 63));
+          if (c + a < n && fc != 0.f)
 #pragma unroll
-          for (int e = 0; e < E; ++e) y[e] += fc * z[a][e];
+            for (int e = 0; e < E; ++e) y[e] += fc * z[a][e];
+        }
       }
     }
-  }
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    ls += __shfl_xor(ls, d);
-    lr += __shfl_xor(lr, d);
+    for (int d = 1; d < 64; d *= 2) {
+      ls += __shfl_xor(ls, d);
+      lr += __shfl_xor(lr, d);
+    }
+    const float inv = inverse(lr);
+    uint16_t *dst = p.o + (int64_t)token * p.o_st + (int64_t)hq * p.o_sh + E * lane;
+    if constexpr (E == 2)
+      *(uint32_t *)dst = pack_bf16(y[0] * inv, y[1] * inv);
+    else
+      *dst = (uint16_t)pack_bf16(y[0] * inv, 0.f);
+    if (p.lse && lane == 0) p.lse[(int64_t)token * p.hq + hq] = lse_of(top, ls);
   }
-  const float inv = inverse(lr);
-  uint16_t *dst = p.o + (int64_t)token * p.o_st + (int64_t)hq * p.o_sh + E * lane;
-  if constexpr (E == 2)
-    *(uint32_t *)dst = pack_bf16(y[0] * inv, y[1] * inv);
-  else
-    *dst = (uint16_t)pack_bf16(y[0] * inv, 0.f);
-  if (p.lse && lane == 0) p.lse[(int64_t)token * p.hq + hq] = lse_of(top, ls);
 }
 
 }  // namespace

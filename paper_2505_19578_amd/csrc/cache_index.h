@@ -30,17 +30,33 @@ constexpr int32_t cache_slot(int64_t page_id, int64_t page, int64_t offset) {
   return page_id < 0 || s > 0x7fffffff ? -1 : (int32_t)s;
 }
 
-// Keys kb .. kb + 31 that new token i of a request sees, as bits.  The request has `ctx` tokens in the cache before its `fresh`
-// new ones; new token j lies at position ctx + j.  words != 0: bit j of mask[] says whether token i sees new token j; words == 0:
-// it sees tokens 0 .. i.  kb may lie anywhere, also behind the last key.
-constexpr uint32_t cache_visible(int64_t kb, int64_t ctx, int fresh, int i, const uint64_t *mask, int words) {
-  uint64_t seen = 0;  // of new tokens kb - ctx, ..
+// Keys kb .. kb + 31 that a new token of a request sees, as bits.  The request has `ctx` tokens in the cache before its `fresh`
+// new ones; new token j lies at position ctx + j.  kb may lie anywhere, also behind the last key.
+//
+// `seen`: bits of new tokens kb - ctx, .. that it sees (of those before the context's end, none count)
+constexpr uint32_t cache_with_context(uint64_t seen, int64_t kb, int64_t ctx) {
+  const int64_t before = ctx - kb;  // keys from kb on that lie in the context
+  const uint64_t old = before <= 0 ? 0 : before >= 32 ? 0xffffffffu : (1ull << before) - 1;
+  return (uint32_t)((seen & ~old) | old);
+}
+constexpr uint64_t cache_low_bits(int64_t n) { return n <= 0 ? 0 : n >= 32 ? 0xffffffffu : (1ull << n) - 1; }
+// New token i of a chain sees tokens 0 .. i.
+constexpr uint32_t cache_visible_chain(int64_t kb, int64_t ctx, int fresh, int i) {
+  const int64_t last = i < fresh ? i : fresh - 1;  // the last new token that is seen
+  return cache_with_context(cache_low_bits(last - (kb - ctx) + 1), kb, ctx);
+}
+// One mask word: bit j says whether the token sees new token j.
+constexpr uint32_t cache_visible_word(int64_t kb, int64_t ctx, int fresh, uint64_t word) {
   const int64_t j0 = kb - ctx;
-  if (words == 0) {
-    const int64_t last = i < fresh ? i : fresh - 1;  // the last new token that is seen
-    const int64_t n = last - j0 + 1;                 // keys from kb on up to it
-    seen = n <= 0 ? 0 : n >= 32 ? 0xffffffffu : (1ull << n) - 1;
-  } else if (j0 < 64 * (int64_t)words && j0 > -32) {
+  uint64_t seen = j0 >= 64 || j0 <= -32 ? 0 : j0 >= 0 ? word >> j0 : word << -j0;
+  seen &= cache_low_bits(fresh - j0);  // keys from kb on that exist
+  return cache_with_context(seen, kb, ctx);
+}
+// Several: bit j % 64 of word j / 64.
+constexpr uint32_t cache_visible_words(int64_t kb, int64_t ctx, int fresh, const uint64_t *mask, int words) {
+  const int64_t j0 = kb - ctx;
+  uint64_t seen = 0;
+  if (j0 < 64 * (int64_t)words && j0 > -32) {
     if (j0 >= 0) {
       const int w = (int)(j0 >> 6), sh = (int)(j0 & 63);
       seen = mask[w] >> sh;
@@ -48,13 +64,9 @@ constexpr uint32_t cache_visible(int64_t kb, int64_t ctx, int fresh, int i, cons
     } else {
       seen = mask[0] << -j0;
     }
-    const int64_t n = fresh - j0;  // keys from kb on that exist
-    seen &= n <= 0 ? 0 : n >= 32 ? 0xffffffffu : (1ull << n) - 1;
+    seen &= cache_low_bits(fresh - j0);
   }
-  const int64_t before = ctx - kb;  // keys from kb on that lie in the context
-  const uint64_t old = before <= 0 ? 0 : before >= 32 ? 0xffffffffu : (1ull << before) - 1;
-  // a new token's key lies behind the context, whatever bits of the chain's rule fall before it
-  return (uint32_t)((seen & ~old) | old);
+  return cache_with_context(seen, kb, ctx);
 }
 
 // One request's share of an attention call: `rows` query rows per KV head in `tiles` tiles, `units` of CACHE_UNIT keys in
@@ -63,13 +75,14 @@ struct CacheShare {
   int32_t first, fresh, keys, rows, tiles, units, chunks;
 };
 // Units of a chunk.  It goes by the request's own sizes alone, so that a request's result is the same bits whatever else the
-// call holds: about 16 chunks per 64 rows, so that one request spreads over the chip, of 2 to 8 units per 64 rows, so that a
-// workgroup has enough to do and a long context still makes more workgroups than 16.
+// call holds: about 16 chunks per 64 rows, so that one request spreads over the chip, of at most 8 units per 64 rows, so that a
+// long context still makes more workgroups than 16, and of at least 2, and one per 32 rows: a chunk's partial results are written
+// and read, 1 KiB a row, next to 64 KiB of keys and values a unit.
 constexpr uint32_t cache_chunk_units(uint32_t units, uint32_t rows) {
-  const uint32_t t = rows > 64 ? (rows + 63) / 64 : 1, most = 8 * t;
+  const uint32_t t = rows > 64 ? (rows + 63) / 64 : 1, most = 8 * t, least = 2 * t;
   if (units >= 128) return most;  // (and 32 bits hold the product below)
   const uint32_t u = (units * t + 15) / 16;
-  return u < 2 ? 2 : u;
+  return u < least ? least : u;
 }
 // Tokens and keys come from device memory: whatever is in it, a share is a share of rows and keys that exist.
 constexpr CacheShare cache_share(int32_t first, int32_t end, int32_t keys, int32_t n_tokens, int32_t most_keys, int32_t group,

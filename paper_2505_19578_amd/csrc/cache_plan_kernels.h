@@ -15,8 +15,7 @@ namespace {
 // launch, with what there is per request kept in LDS; beyond, the second part is spread over the chip.
 constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64;
 constexpr int PLAN_ONE_LAUNCH = 4096;           // tokens
-constexpr int PLAN_PART_THREADS = 256;          // of the second part's own launch
-constexpr int PLAN_PART_TOKENS = 1024;          // tokens of its workgroup
+constexpr int PLAN_PART_THREADS = 256;          // and tokens of a workgroup, of the second part's own launch
 constexpr int PLAN_MAX_TREE = 64 * CACHE_MAX_WORDS;
 
 struct PlanParams {
@@ -126,13 +125,22 @@ __device__ __forceinline__ void plan_tokens(const PlanParams &p, int n_free, int
             m[w] = n < 0 ? 0ull : n >= 63 ? ~0ull : (2ull << n) - 1;
           }
         } else if (p.words) {
+          const int16_t *mine = up + (first - up0);
           depth = -1;
-          for (int a = i; a >= 0; ++depth) {
+          auto walk = [&](auto &&mark) {
+            for (int a = i; a >= 0; ++depth) {
+              const int q2 = mine[a];
+              mark(a);
+              a = q2 < a ? q2 : -1;  // no earlier token of the request: a root
+            }
+          };
+          if (p.words == 1)
+            walk([&](int a) { m[0] |= 1ull << a; });
+          else
+            walk([&](int a) {
 #pragma unroll
-            for (int w = 0; w < CACHE_MAX_WORDS; ++w) m[w] |= (a >> 6) == w ? 1ull << (a & 63) : 0ull;
-            const int q2 = up[first + a - up0];
-            a = q2 < a ? q2 : -1;  // no earlier token of the request: a root
-          }
+              for (int w = 0; w < CACHE_MAX_WORDS; ++w) m[w] |= (a >> 6) == w ? 1ull << (a & 63) : 0ull;
+            });
         } else {  // positions alone: a tree of any size, by its own memory
           for (int a = i;; ++depth) {
             const int q2 = p.parents[first + a];
@@ -182,8 +190,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(PlanParams p, int wi
 }
 
 __global__ __launch_bounds__(PLAN_PART_THREADS) void plan_tokens_kernel(PlanParams p) {
-  __shared__ int16_t up[PLAN_PART_TOKENS + PLAN_MAX_TREE];
-  const int t0 = blockIdx.x * PLAN_PART_TOKENS, t1 = min(p.max_tokens, t0 + PLAN_PART_TOKENS), up0 = max(0, t0 - PLAN_MAX_TREE);
+  __shared__ int16_t up[PLAN_PART_THREADS + PLAN_MAX_TREE];
+  const int t0 = blockIdx.x * PLAN_PART_THREADS, t1 = min(p.max_tokens, t0 + PLAN_PART_THREADS), up0 = max(0, t0 - PLAN_MAX_TREE);
   if (p.parents && p.words) {
     for (int t = up0 + (int)threadIdx.x; t < t1; t += PLAN_PART_THREADS) up[t - up0] = short_parent(p.parents[t]);
     __syncthreads();

@@ -33,7 +33,8 @@ def test_visible_keys_of_a_step(tmp_path, words):
             if (i >= fresh) continue;
             const int64_t from = ctx / 32 * 32 - 64;
             for (int64_t kb = from < 0 ? 0 : from; kb <= (int64_t)ctx + fresh + 64; kb += 32) {{
-              const uint32_t got = cache_visible(kb, ctx, fresh, i, mask, words);
+              const uint32_t got = words ? cache_visible_words(kb, ctx, fresh, mask, words) : cache_visible_chain(kb, ctx, fresh, i);
+              if (words == 1 && got != cache_visible_word(kb, ctx, fresh, mask[0])) return 2;
               for (int b = 0; b < 32; ++b) {{
                 const int64_t j = kb + b - ctx;
                 const bool want = j < 0 || (j < fresh && (words ? (mask[j / 64] >> (j % 64)) & 1 : j <= i));
