@@ -754,6 +754,7 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
         pf[c] = rows.weights_of(pairs[c]);
       }
       if (s + 1 >= soft) hide(s + 1, next);
+      __builtin_amdgcn_s_setprio(1);  // the other workgroup's vector work goes beside it: 3 % of a tree over 128K
       rows.add_ones(pf);
       groups_read_ahead<DT>([&](int d) { return v_fragment(slot_of(s), d); },
                             [&](auto dc, const bf16x8 &a) __attribute__((always_inline)) {
@@ -765,6 +766,7 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
           for (int e = 8 / DT * d; e < 8 / DT * (d + 1); ++e) top[c] = e ? fmaxf(top[c], next[e / 4][c][e % 4]) : next[0][c][0];
         }
       });
+      __builtin_amdgcn_s_setprio(0);
     };
     rows.clear();
     if (steps > 0) {
@@ -784,11 +786,10 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
         rows.largest(even, top);
       }
       for (int s = 0; s < steps; s += 2) {
-        // K of steps s + 1 and s + 2 and V of steps s and s + 1 have arrived, and nobody reads what came before
-        if (s) {
-          wait_copies<0>();
-          __syncthreads();
-        }
+        // K of steps s + 1 and s + 2 and V of steps s and s + 1 have arrived, and nobody reads what came before (the first time: K
+        // of step 0, in whose place that of step 4 goes)
+        wait_copies<0>();
+        __syncthreads();
         if (s + 2 < steps) {
           if (s + 4 - from_step >= 64) load_places(s + 2);
           fetch_k(s + 3);
