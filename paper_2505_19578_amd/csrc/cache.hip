@@ -103,10 +103,13 @@ int log2_of(int32_t x) { return __builtin_ctz((unsigned)x); }
 size_t plan_bytes(int32_t n) { return ((size_t)2 * n + 1) * sizeof(int32_t); }
 
 // ------------------------------------------------------------------------------------------------------------- attention
-// Rows of a workgroup's tile, by the rows (group * max_new) that a request has under one KV head.
+// Rows of a workgroup's tile, by the rows (group * max_new) that a request has under one KV head.  Up to 16 the narrow kernel: 64
+// contexts of 8K with 4 rows 412 us and 414 in the wide one, 32 of 3000 with 8 rows 95 and 103, 16 of 500 with 4 16.8 and 18.4
+// (one of 100K 99 and 97).  Two column groups to a wavefront from 65 on: a key's fragment is read from LDS once for 32 rows
+// instead of 16.
 int attn_tile_rows(const sp_step_shape *s, const sp_cache_shape *c) {
   const int64_t rows = (int64_t)s->max_new * (s->n_q_heads / c->n_kv_heads);
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  return rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
 }
 int64_t attn_most_keys(const sp_step_shape *s, const sp_cache_shape *c) { return (int64_t)s->max_pages * c->page_size; }
 int64_t attn_partial_rows(const sp_step_shape *s, const sp_cache_shape *c) {
@@ -152,9 +155,7 @@ template <int D>
 sp_status launch_cache_attn(const CacheAttnParams &p, int tile_rows, int64_t items, hipStream_t st) {
   const dim3 grid((unsigned)std::min(items, CA_GRID)), block(CA_THREADS);
   if (tile_rows == 16)
-    hipLaunchKernelGGL((cache_attn_narrow_kernel<D, 1>), grid, block, 0, st, p);
-  else if (tile_rows == 32)
-    hipLaunchKernelGGL((cache_attn_narrow_kernel<D, 2>), grid, block, 0, st, p);
+    hipLaunchKernelGGL((cache_attn_narrow_kernel<D>), grid, block, 0, st, p);
   else if (tile_rows == 64)
     hipLaunchKernelGGL((cache_attn_wide_kernel<D, 1>), grid, block, 0, st, p);
   else

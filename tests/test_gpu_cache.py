@@ -508,3 +508,225 @@ def test_accept_of_nothing():
     sp.sp_cache_accept(sp.cache_shape_of(k), k, k, _i32([[0, 1]]), _i32([-7]), _i32([20]), torch.zeros(1, 0, dtype=torch.int32, device="cuda"),
                        _i32([5]), out)
     assert torch.equal(k, before) and out.item() == -7
+
+
+# ------------------------------------------------------------------------------------------------------------------ together
+class _Server:
+    """A batch of requests, a few layers, and device buffers that a step reuses: what a serving loop keeps."""
+
+    def __init__(self, n, layers, hq, hk, d, page, width, words, tokens, seed):
+        import torch
+        sp = _sp()
+        g = torch.Generator().manual_seed(seed)
+        i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.dims, self.words, self.layers, self.tokens = (hq, hk, d, page), words, layers, tokens
+        pages = n * width
+        self.k, self.v = (torch.full((layers, pages, page, hk, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        self.cache = sp.cache_shape_of(self.k[0])
+        self.ctx, self.new, self.held, self.seq, self.status, self.after = (i32(n) for _ in range(6))
+        self.table, self.start = torch.full((n, width), -1, dtype=torch.int32, device="cuda"), i32(n + 1)
+        self.free = torch.randperm(pages, generator=g).to(torch.int32).cuda()
+        self.n_free = _i32([pages])
+        self.pos, self.slots, self.parents = i32(tokens), i32(tokens), i32(tokens)
+        self.mask = torch.zeros((tokens, words), dtype=torch.int64, device="cuda")
+        self.qkv = torch.zeros((layers, tokens, hq + 2 * hk, d), dtype=torch.bfloat16, device="cuda")
+        self.q = torch.zeros((layers, tokens, hq, d), dtype=torch.bfloat16, device="cuda")
+        self.o, self.lse = torch.zeros_like(self.q), torch.zeros((layers, tokens, hq), device="cuda")
+        self.w = [(torch.rand(d, generator=g) + 0.5).to(torch.bfloat16).cuda() for _ in range(2)]
+        self.inv = (10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).float().cuda()
+        self.path, self.count = i32(n, 4), i32(n)
+        self.shape = sp.step_shape_of(self.q[0], self.o[0], self.table, 64 * words, words)
+        self.ws = torch.empty(max(sp.sp_cache_attn_workspace_bytes(self.shape, self.cache), sp.sp_cache_plan_workspace_bytes(n)),
+                              dtype=torch.uint8, device="cuda")
+
+    def step(self):
+        """Plan, every layer, and what the (already known) acceptance keeps: device work only."""
+        sp = _sp()
+        hq, hk, d, page = self.dims
+        sp.sp_cache_plan(self.ctx, self.new, self.held, self.table, self.free, self.n_free, page, self.parents, self.held, self.n_free,
+                         self.start, self.seq, self.pos, self.slots, self.status, self.mask, self.ws)
+        for l in range(self.layers):
+            q, k, v = (self.qkv[l, :, a:b] for a, b in ((0, hq), (hq, hq + hk), (hq + hk, hq + 2 * hk)))
+            sp.sp_qk_norm_rope(sp.rope_shape_of(q, k, v, self.q[l], None, d), q, k, v, self.w[0], self.w[1], self.inv, self.pos, self.q[l],
+                               None, self.cache, self.k[l], self.v[l], self.slots)
+            sp.sp_cache_attn(self.shape, self.cache, self.q[l], self.k[l], self.v[l], self.table, self.seq, self.start, self.mask,
+                             self.o[l], self.lse[l], self.ws)
+        sp.sp_cache_accept(self.cache, self.k, self.v, self.table, self.ctx, self.seq, self.path, self.count, self.after)
+        self.ctx.copy_(self.after)
+
+    def ask(self, new, parents, path, count, seed):
+        """The next step's tokens into the buffers; rows behind the last token hold NaN."""
+        import torch
+        g = torch.Generator().manual_seed(seed)
+        n = sum(new)
+        self.new.copy_(_i32(new))
+        self.parents.copy_(_i32(parents + [-1] * (self.tokens - n)))
+        x = torch.randn(self.qkv.shape, generator=g) * 1.5
+        x[:, n:] = float("nan")
+        self.qkv.copy_(x.to(torch.bfloat16).cuda())
+        self.path.copy_(_i32(path))
+        self.count.copy_(_i32(count))
+
+
+def _steps(seed, n, steps):
+    """Random steps: lengths, trees, and paths down them that are kept."""
+    rng = np.random.default_rng(seed)
+    out = []
+    for _ in range(steps):
+        new = rng.integers(0, 12, n).tolist()
+        parents, path, count = [], [], []
+        for t in new:
+            p = [-1] + [int(rng.integers(max(0, i - 3), i)) for i in range(1, t)]
+            parents += p[:t]
+            down = []
+            at = t - 1
+            while at >= 0:
+                down.append(at)
+                at = p[at]
+            down = down[::-1][:4]
+            path.append(down + [-1] * (4 - len(down)))
+            count.append(len(down))
+        out.append((new, parents, path, count))
+    return out
+
+
+def test_a_serving_loop_against_the_reference():
+    """Five steps of drafted trees over two layers: what the steps leave in tables and caches is what the next ones read."""
+    import torch
+    from oracle import cache as oracle
+    n, layers, hq, hk, d, page, width, words, tokens = 5, 2, 6, 2, 64, 16, 6, 1, 64
+    s = _Server(n, layers, hq, hk, d, page, width, words, tokens, 3)
+    free, n_free, ctx, held = _host(s.free), n * width, np.zeros(n, int), np.zeros(n, int)
+    table = np.full((n, width), -1)
+    k, v = (np.full((layers, n * width, page, hk, d), np.nan) for _ in range(2))
+    for number, (new, parents, path, count) in enumerate(_steps(5, n, 5)):
+        print(f"[loop] step {number}: {new}", flush=True)
+        s.ask(new, parents, path, count, 100 + number)
+        before = s.ctx.clone()
+        s.step()
+        plan = oracle.plan(ctx, new, held, table, free, n_free, page, tokens, np.array(parents + [-1] * 64), words)
+        assert np.array_equal(_host(s.slots), plan["slots"]) and np.array_equal(_host(s.table), plan["table"])
+        assert np.array_equal(_host(before), ctx) and int(s.n_free[0]) == plan["n_free"]
+        used = plan["tok_start"][-1]
+        for l in range(layers):
+            x = _host(s.qkv[l])
+            for part, w, got in (("q", s.w[0], s.q[l]), ("k", s.w[1], None)):
+                a, b = (0, hq) if part == "q" else (hq, hq + hk)
+                want, size = oracle.norm_rope(x[:used, a:b], _host(w), 1e-6, plan["positions"][:used], _host(s.inv), d, False)
+                if part == "q":
+                    assert (np.abs(_host(got)[:used] - want) <= HALF_BF16 * np.abs(want) + 2.0 ** -16 * size).all()
+                else:   # the reference goes on with the library's rounding of the keys, which is checked here
+                    rows = torch.stack([s.k[l].view(-1, hk, d)[t] for t in plan["slots"][:used].tolist()]) if used else s.k[l].view(-1, hk, d)[:0]
+                    moved = {int(plan["slots"][t]) for r in range(n) for t in range(plan["tok_start"][r], plan["tok_start"][r] + count[r])}
+                    for t in range(used):
+                        flat = (l, int(plan["slots"][t]) // page, int(plan["slots"][t]) % page)
+                        if int(plan["slots"][t]) not in moved:
+                            assert (np.abs(_host(rows[t]) - want[t]) <= HALF_BF16 * np.abs(want[t]) + 2.0 ** -16 * size[t]).all()
+                        k[flat] = torch.from_numpy(want[t]).to(torch.bfloat16).double().numpy()
+                        v[flat] = x[t, hq + hk:]
+            q = _host(s.q[l])
+            o, lse, big, _ = oracle.attention(q, np.nan_to_num(k[l]), np.nan_to_num(v[l]), plan["table"], plan["seq_len"], plan["tok_start"],
+                                              plan["mask"], d ** -0.5)
+            # the keys' rounding differs from the reference's where a value lies next to a border: half a step of each, through
+            # the softmax at most twice that of the logits' size, which is below 40 here
+            err = np.abs(_host(s.o[l])[:used] - o[:used])
+            assert (err <= (3 * HALF_BF16 + 0.02) * big[:used] + 1e-6).all(), err.max()
+        kept = oracle.accept(k, v, plan["table"], ctx, plan["seq_len"], path, count)
+        ctx, held, table, n_free = kept, plan["n_held"], plan["table"], plan["n_free"]
+        assert np.array_equal(_host(s.ctx), ctx)
+
+
+def test_a_captured_step_replays_with_other_lengths():
+    """One graph of a whole step, its state updated in place: replays with other tokens, eager work and synchronisations between,
+    against the same steps made eagerly; and rows behind the last token write nothing."""
+    import torch
+    args = (4, 2, 8, 2, 128, 16, 8, 1, 60)
+    eager, graphed = _Server(*args, 9), _Server(*args, 9)
+    state = lambda s: [s.ctx, s.held, s.n_free, s.table, s.k, s.v, s.slots, s.pos, s.mask, s.status]  # noqa: E731
+    keep = [t.clone() for t in state(graphed)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graphed.step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        graphed.step()
+    for a, b in zip(state(graphed), keep):
+        a.copy_(b)
+    for number, asked in enumerate(_steps(6, 4, 4)):
+        print(f"[graph] replay {number}: {asked[0]}", flush=True)
+        eager.ask(*asked, 200 + number)
+        graphed.ask(*asked, 200 + number)
+        eager.step()
+        graph.replay()
+        torch.cuda.synchronize()
+        used = int(eager.start[-1])
+        assert torch.equal(eager.start, graphed.start)
+        for a, b in zip(state(eager) + [eager.o[:, :used], eager.lse[:, :used]], state(graphed) + [graphed.o[:, :used], graphed.lse[:, :used]]):
+            assert torch.equal(a.view(torch.int16) if a.dtype is torch.bfloat16 else a, b.view(torch.int16) if b.dtype is torch.bfloat16 else b)
+        assert (graphed.slots[used:] == -1).all()
+        assert np.isfinite(torch.randn(1 << 16, device="cuda").sum().item())
+
+
+def test_calls_on_two_streams():
+    """A call runs on the stream that is current, whatever stream made its inputs, and two at once with workspaces of their own do
+    not meet."""
+    import torch
+    sp = _sp()
+    cases = [_step([3000, 200], [4, 3], 8, 2, 128, 16, 1, 31), _step([100, 2500], [3, 4], 8, 2, 128, 16, 1, 32)]
+    want = [_attend(c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    made = []
+    for c, st in zip(cases, streams):
+        q, k, v, table, seq, start, mask = (c["q"].cuda(), c["k"].cuda(), c["v"].cuda(), _i32(c["table"]), _i32(c["seq"]), _i32(c["start"]),
+                                            _words(c["mask"]))
+        o, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+        shape, cache = sp.step_shape_of(q, o, table, c["top"], 1), sp.cache_shape_of(k)
+        ws = torch.empty(sp.sp_cache_attn_workspace_bytes(shape, cache), dtype=torch.uint8, device="cuda")
+        made.append((shape, cache, q, k, v, table, seq, start, mask, o, lse, ws))
+        st.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for m, st in zip(made, streams):
+            with torch.cuda.stream(st):
+                m[9].fill_(3)
+                sp.sp_cache_attn(*m)
+    torch.cuda.synchronize()
+    for m, (o, lse) in zip(made, want):
+        assert np.array_equal(_host(m[9]), o) and np.array_equal(_host(m[10]), lse)
+
+
+def test_a_prefill_and_the_steps_after_it():
+    """A prompt's rows go through sp_qk_norm_rope into sp_dense_attn_with_block_scores and into the cache; the same prompt's last
+    tokens asked again over the cache get what the prefill gave them."""
+    import torch
+    sp = _sp()
+    seq, hq, hk, d, page, last = 512, 8, 2, 128, 64, 9
+    torch.manual_seed(4)
+    qkv = torch.randn(seq, hq + 2 * hk, d, device="cuda").to(torch.bfloat16)
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:]
+    w = torch.rand(d, device="cuda").add(0.5).to(torch.bfloat16)
+    inv = (10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).float().cuda()
+    ctx, new, held, start, length, status = (_i32(x) for x in ([0], [seq], [0], [0, 0], [0], [0]))
+    table, free, n_free = torch.full((1, 16), -1, dtype=torch.int32, device="cuda"), _i32(np.random.default_rng(1).permutation(16)), _i32([16])
+    pos, slots = torch.empty(seq, dtype=torch.int32, device="cuda"), torch.empty(seq, dtype=torch.int32, device="cuda")
+    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    sp.sp_cache_plan(ctx, new, held, table, free, n_free, page, None, held, n_free, start, length, pos, slots, status, None, ws)
+    kc, vc = (torch.zeros(16, page, hk, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    qr, kr = torch.empty(seq, hq, d, dtype=torch.bfloat16, device="cuda"), torch.empty(seq, hk, d, dtype=torch.bfloat16, device="cuda")
+    sp.sp_qk_norm_rope(sp.rope_shape_of(q, k, v, qr, kr, d), q, k, v, w, w, inv, pos, qr, kr, sp.cache_shape_of(kc), kc, vc, slots)
+    shape = sp.shape_of(qr[None], kr[None], None, 128)
+    o = torch.empty_like(qr)
+    big = torch.empty(sp.sp_workspace_bytes(shape, 0), dtype=torch.uint8, device="cuda")
+    vp = v.contiguous()
+    assert vp.stride() == kr.stride()
+    sp.sp_dense_attn_with_block_scores(shape, qr, kr, vp, list(range(hq)), o, None, big)
+    ql, ol = qr[-last:], torch.empty(last, hq, d, dtype=torch.bfloat16, device="cuda")
+    step, cache = sp.step_shape_of(ql, ol, table, last), sp.cache_shape_of(kc)
+    ws = torch.empty(sp.sp_cache_attn_workspace_bytes(step, cache), dtype=torch.uint8, device="cuda")
+    sp.sp_cache_attn(step, cache, ql, kc, vc, table, length, _i32([0, last]), None, ol, None, ws)
+    # both round weights (2^-8 each, in the sum and its normaliser) and result (2^-8): twice 3 * 2^-8 of sum p |v|, which the mean |v|
+    # of a row's 500 keys, below 1.2 here, bounds
+    err = (ol.float() - o[-last:].float()).abs().max().item()
+    assert err <= 2 * 3 * HALF_BF16 * 1.2, err
