@@ -412,6 +412,7 @@ sp_status sp_prefill_layer_dict(const sp_shape *shape, const void *q, const void
  *
  * Envelope: bf16, head_dim 64 or 128, page_size a power of two from 16 to 4096, n_pages * page_size and max_pages * page_size
  * below 2^31, stride_token at most 2^24, at most 2^20 requests and 2^28 tokens in a call, no tokens or no requests allowed.
+ * Calls that may run at the same time, in captured graphs too, need workspaces of their own.
  * These calls are not bracketed by sp_profile_enable.
  */
 typedef struct {
@@ -448,7 +449,8 @@ sp_status sp_cache_plan_workspace_bytes(int32_t n_requests, size_t *bytes);
  *   block_table                device int32 [n_requests][max_pages]    (input and output)
  *   free_pages                 device int32 [free_capacity]; n_free: device int32 [1]
  *   parents                    device int32 [max_tokens], packed: the parent of a new token, counted from its request's first;
- *                              -1 (and whatever is not an earlier token): none.  NULL: every request's tokens are a chain
+ *                              -1 (and whatever is not an earlier token): none.  NULL: every request's tokens are a chain.
+ *                              Without masks a tree may have any size, and every token takes a load per step up to its root
  *   n_held_out, n_free_out     device int32 [n_requests], [1]; may be n_held's and n_free's own memory
  *   tok_start, seq_len, status device int32 [n_requests + 1], [n_requests], [n_requests]  (outputs; distinct memory)
  *   positions, slots           device int32 [max_tokens]               (outputs)
@@ -484,7 +486,7 @@ typedef struct {
  *   q_out               device bf16; may be q's memory with q's strides
  *   k_out               device bf16 or NULL (only the cache); may be k's memory with k's strides
  *   cache               NULL (no cache), or its geometry with k_cache, v_cache and slots (device int32 [n_tokens]); two tokens
- *                       with one slot: which of them stays is not said
+ *                       with one slot: which of them, or what parts of each, stay there is not said
  */
 sp_status sp_qk_norm_rope(const sp_rope_shape *shape, const void *q, const void *k, const void *v, const void *q_weight,
                           const void *k_weight, const float *inv_freq, const int32_t *positions, void *q_out, void *k_out,
@@ -512,10 +514,12 @@ sp_status sp_cache_attn_workspace_bytes(const sp_step_shape *shape, const sp_cac
  * A row that sees no key (a refused request, pages that do not exist, an empty mask) gets o = 0 and lse = -inf.  Keys and values
  * that a row does not see do not touch it, whatever they hold (NaN and infinities among them).  Rows of o and lse behind
  * tok_start[n_requests] are left as they were.  A request with seq_len below its number of new tokens counts as refused.
- * tok_start that falls anywhere: nothing is written.
+ * Where tok_start falls, the rows of the requests from there on are unspecified; nothing outside them is touched.
+ * A request's rows have the same bits whatever else the call holds, at which places its pages lie and however often it is made,
+ * as long as max_new * n_q_heads / n_kv_heads stays on one side of 16 (1 to 16: kernel for few rows; more: for many).
  *   q           device bf16 [n_tokens][n_q_heads][head_dim] (strides as given)
  *   k_cache, v_cache, block_table, seq_len, tok_start, tree_mask  as sp_cache_plan and sp_qk_norm_rope leave them
- *   o           device bf16 (output);  lse: device fp32 [n_tokens][n_q_heads] or NULL (output)
+ *   o           device bf16 (output; not q's memory);  lse: device fp32 [n_tokens][n_q_heads] or NULL (output)
  *   workspace   sp_cache_attn_workspace_bytes(shape, cache)
  */
 sp_status sp_cache_attn(const sp_step_shape *shape, const sp_cache_shape *cache, const void *q, const void *k_cache,
@@ -530,7 +534,7 @@ sp_status sp_cache_attn(const sp_step_shape *shape, const sp_cache_shape *cache,
  * not below seq_len - ctx_len.  ctx_out = ctx_len + entries of the path.  A move from or to a page that does not exist is left out.
  *   k_cache, v_cache       device bf16, n_layers caches of the given geometry, stride_layer elements apart
  *   ctx_len, seq_len, n_accepted  device int32 [n_requests];  path: device int32 [n_requests][max_accept], max_accept <= 256
- *   ctx_out                device int32 [n_requests] or NULL; not ctx_len's or seq_len's memory
+ *   ctx_out                device int32 [n_requests] or NULL; no other argument's memory
  */
 sp_status sp_cache_accept(const sp_cache_shape *cache, int32_t n_layers, int64_t stride_layer, void *k_cache, void *v_cache,
                           int32_t n_requests, int32_t max_pages, const int32_t *block_table, const int32_t *ctx_len,

@@ -192,6 +192,8 @@ def sp_cache_attn(shape: SpStepShape, cache: SpCacheShape, q, k_cache, v_cache, 
                   lse, workspace):
     """tree_mask None with mask_words 0; lse None: not wanted."""
     s, dev = shape, q.get_device()
+    if tree_mask is not None and tree_mask.shape[-1] != s.mask_words:
+        raise ValueError(f"tree_mask has {tree_mask.shape[-1]} words a token, the shape {s.mask_words}")
     n, rows = s.n_requests, (s.n_tokens, s.n_q_heads, cache.head_dim)
     _call(lib().sp_cache_attn, dev, ctypes.byref(s), ctypes.byref(cache), _rows(q, rows, (s.q_stride_t, s.q_stride_h, 1), dev, "q"),
           _cache_rows(cache, k_cache, dev, "k_cache"), _cache_rows(cache, v_cache, dev, "v_cache"),

@@ -346,8 +346,8 @@ sp_status sp_cache_accept(const sp_cache_shape *cache, int32_t n_layers, int64_t
       (rc = may(ctx_out, 4, "ctx_out")))
     return rc;
   if (max_accept > 0 && (rc = need(path, 4, "path"))) return rc;
-  if (ctx_out && (ctx_out == ctx_len || ctx_out == seq_len))
-    return fail(SP_ERR_INVALID_ARG, "ctx_out must not be ctx_len's or seq_len's memory");
+  if (ctx_out && (ctx_out == ctx_len || ctx_out == seq_len || ctx_out == n_accepted || ctx_out == path || ctx_out == block_table))
+    return fail(SP_ERR_INVALID_ARG, "ctx_out must be no other argument's memory");  // other workgroups of the request read those
   AcceptParams p{};
   p.k = (uint16_t *)k_cache, p.v = (uint16_t *)v_cache;
   p.table = block_table, p.ctx = ctx_len, p.seq = seq_len, p.path = path, p.count = n_accepted, p.ctx_out = ctx_out;

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(ACCEPT_THREADS) void cache_accept_kernel(AcceptPara
   const int ctx = p.ctx[r];
   // the path ends at the first entry that does not ascend or is no new token of the request
   if (tid < 64) {
-    const int fresh = ctx < 0 ? 0 : p.seq[r] - ctx;
+    const int seq = p.seq[r], fresh = ctx < 0 || seq < ctx ? 0 : seq - ctx;
     int n = p.count[r], prev = -1;
     n = n < 0 ? 0 : n > p.max_accept ? p.max_accept : n;
     int len = 0;

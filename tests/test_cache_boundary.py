@@ -204,6 +204,15 @@ def test_accept_arguments():
     _said(call(n=0, **{x: None for x in names}), "SP_OK")
 
 
+@pytest.mark.parametrize("where", ["block_table", "ctx_len", "seq_len", "path", "n_accepted"])
+def test_accept_does_not_write_what_it_reads(where):
+    """Workgroups of one request (layers, pieces of a row) read these while the first of them writes ctx_out."""
+    L, c, at = sp.lib(), _cache(), dict(block_table=2, ctx_len=3, seq_len=4, path=5, n_accepted=6)
+    a = [FAKE + 512 * i for i in range(8)]
+    rc = L.sp_cache_accept(ctypes.byref(c), 3, 8 * 16 * 128, a[0], a[1], 2, 4, a[2], a[3], a[4], 5, a[5], a[6], a[at[where]], None)
+    _said(rc, "SP_ERR_INVALID_ARG", b"ctx_out")
+
+
 def test_binding_refuses_host_memory_and_other_sizes():
     """The binding looks at the tensors before the library sees an address: a host tensor's would fault the device."""
     import torch
@@ -229,5 +238,7 @@ def test_binding_refuses_host_memory_and_other_sizes():
                          i32(2), None, ws)
     with pytest.raises(ValueError, match="on cpu"):
         sp.sp_cache_accept(c, cache, cache, i32(2, 3), i32(2), i32(2), i32(2, 4), i32(2))
+    with pytest.raises(ValueError, match="words a token"):
+        sp.sp_cache_attn(s, c, q, cache, cache, i32(2, 3), i32(2), i32(3), torch.zeros(2, 1, dtype=torch.int64), q, None, ws)
     with pytest.raises(ValueError, match="one geometry"):
         sp.sp_cache_accept(c, cache, cache[None], i32(2, 3), i32(2), i32(2), i32(2, 4), i32(2))

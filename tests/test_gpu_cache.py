@@ -510,6 +510,17 @@ def test_accept_of_nothing():
     assert torch.equal(k, before) and out.item() == -7
 
 
+def test_accept_of_lengths_far_apart():
+    """seq_len - ctx_len of a refused or overwritten request may pass 32 bits: it has no new tokens then, and nothing moves."""
+    import torch
+    sp = _sp()
+    k = torch.arange(4 * 16 * 64, device="cuda").remainder(251).to(torch.bfloat16).reshape(4, 16, 1, 64)
+    was, low, out = k.clone(), -2**31, _i32([9, 9, 9, 9])
+    sp.sp_cache_accept(sp.cache_shape_of(k), k, k, _i32([[0, 1], [1, 2], [2, 3], [3, 0]]), _i32([1, 7, low, 3]), _i32([low, 0, 2**31 - 1, 2]),
+                       _i32([[2, 3]] * 4), _i32([2] * 4), out)
+    assert out.tolist() == [1, 7, low, 3] and torch.equal(k, was)
+
+
 # ------------------------------------------------------------------------------------------------------------------ together
 class _Server:
     """A batch of requests, a few layers, and device buffers that a step reuses: what a serving loop keeps."""
