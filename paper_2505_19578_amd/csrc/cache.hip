@@ -113,10 +113,10 @@ int attn_tile_rows(const sp_step_shape *s, const sp_cache_shape *c) {
 }
 int64_t attn_most_keys(const sp_step_shape *s, const sp_cache_shape *c) { return (int64_t)s->max_pages * c->page_size; }
 int64_t attn_partial_rows(const sp_step_shape *s, const sp_cache_shape *c) {
-  return c->n_kv_heads * cache_partial_rows(s->n_requests, s->n_tokens, s->n_q_heads / c->n_kv_heads, attn_most_keys(s, c));
+  return c->n_kv_heads * cache_partial_rows(s->n_requests, s->n_tokens, s->n_q_heads / c->n_kv_heads, attn_most_keys(s, c), c->n_kv_heads);
 }
 int64_t attn_items(const sp_step_shape *s, const sp_cache_shape *c) {
-  return c->n_kv_heads * cache_grid(s->n_requests, s->n_tokens, s->n_q_heads / c->n_kv_heads, attn_most_keys(s, c), attn_tile_rows(s, c));
+  return c->n_kv_heads * cache_grid(s->n_requests, s->n_tokens, s->n_q_heads / c->n_kv_heads, attn_most_keys(s, c), attn_tile_rows(s, c), c->n_kv_heads);
 }
 size_t attn_bytes(const sp_step_shape *s, const sp_cache_shape *c) {
   return (size_t)attn_partial_rows(s, c) * (c->head_dim + 4) * sizeof(float);
@@ -161,7 +161,7 @@ sp_status launch_cache_attn(const CacheAttnParams &p, int tile_rows, int64_t ite
   else
     hipLaunchKernelGGL((cache_attn_wide_kernel<D, 2>), grid, block, 0, st, p);
   const sp_status rc = launched("cache_attn_kernel");
-  if (rc || cache_most_chunks(p.most_keys) == 1) return rc;  // no request has two chunks
+  if (rc || cache_most_chunks(p.most_keys, p.hk) == 1) return rc;  // no request has two chunks
   const int64_t rows = (int64_t)p.n_tok * p.hq;
   hipLaunchKernelGGL((cache_join_kernel<D>), dim3((unsigned)std::min((rows + CA_WAVES - 1) / CA_WAVES, CA_GRID)), block, 0, st, p);
   return launched("cache_join_kernel");
@@ -319,7 +319,7 @@ sp_status sp_cache_attn(const sp_step_shape *shape, const sp_cache_shape *cache,
   p.c_sp = c.stride_page, p.c_st = c.stride_token, p.c_sh = c.stride_head;
   p.most_keys = (int)attn_most_keys(shape, cache);
   p.n_req = s.n_requests, p.n_tok = s.n_tokens, p.hq = s.n_q_heads, p.hk = c.n_kv_heads, p.group = s.n_q_heads / c.n_kv_heads;
-  p.page_shift = log2_of(c.page_size), p.n_pages = c.n_pages, p.width = s.max_pages, p.words = s.mask_words;
+  p.page_shift = log2_of(c.page_size), p.n_pages = c.n_pages, p.width = s.max_pages, p.words = s.mask_words, p.many_split = cache_many_split(c.n_kv_heads);
   const float scale = s.softmax_scale > 0.f ? s.softmax_scale : 1.0f / sqrtf((float)c.head_dim);
   p.c = scale * 1.4426950408889634f;
   const int rows = attn_tile_rows(shape, cache);

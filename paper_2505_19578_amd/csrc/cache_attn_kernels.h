@@ -33,7 +33,7 @@ struct CacheAttnParams {
   float *part_o, *part_ml;  // [partial rows][D], [partial rows][4]: reference, sum, sum of rounded weights
   int64_t q_st, q_sh, o_st, o_sh, c_sp, c_st, c_sh;
   int most_keys;
-  int n_req, n_tok, hq, hk, group, page_shift, n_pages, width, words;
+  int n_req, n_tok, hq, hk, group, page_shift, n_pages, width, words, many_split;
   float c;  // softmax scale * log2(e)
 };
 
@@ -70,7 +70,7 @@ struct CacheWalk {
     const int r = r0 + lane;
     const bool live = r < p.n_req;
     first = live ? p.start[r] : 0, end = live ? p.start[r + 1] : 0, keys = live ? p.seq[r] : 0;
-    const CacheShare s = cache_share(first, end, keys, p.n_tok, p.most_keys, p.group, TILE);
+    const CacheShare s = cache_share(first, end, keys, p.n_tok, p.most_keys, p.group, TILE, p.hk, p.many_split);
     good = !any_lane(end < first);  // otherwise this is no tok_start: nothing behind is done, so that no index leaves its buffer
     upto = items + (int)wave_prefix((uint32_t)(s.tiles * p.hk * s.chunks));
     parts = rows + (int)wave_prefix((uint32_t)(s.chunks > 1 ? s.rows * p.hk * s.chunks : 0));
@@ -84,7 +84,7 @@ struct CacheWalk {
       if (hit) {
         const int at = __builtin_ctzll(hit);
         auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-        out.s = cache_share(of(first), of(end), of(keys), p.n_tok, p.most_keys, p.group, TILE);
+        out.s = cache_share(of(first), of(end), of(keys), p.n_tok, p.most_keys, p.group, TILE, p.hk, p.many_split);
         out.r = r0 + at;
         out.items_before = of(upto) - out.s.tiles * p.hk * out.s.chunks;
         out.rows_before = of(parts) - (out.s.chunks > 1 ? out.s.rows * p.hk * out.s.chunks : 0);

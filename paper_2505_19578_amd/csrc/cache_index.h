@@ -74,19 +74,28 @@ constexpr uint32_t cache_visible_words(int64_t kb, int64_t ctx, int fresh, const
 struct CacheShare {
   int32_t first, fresh, keys, rows, tiles, units, chunks;
 };
-// Units of a chunk.  It goes by the request's own sizes alone, so that a request's result is the same bits whatever else the
-// call holds: about 16 chunks per 64 rows, so that one request spreads over the chip, of at most 8 units per 64 rows, so that a
-// long context still makes more workgroups than 16, and of at least 2, and one per 32 rows: a chunk's partial results are written
-// and read, 1 KiB a row, next to 64 KiB of keys and values a unit.
-constexpr uint32_t cache_chunk_units(uint32_t units, uint32_t rows) {
-  const uint32_t t = rows > 64 ? (rows + 63) / 64 : 1, most = 8 * t, least = 2 * t;
-  if (units >= 128) return most;  // (and 32 bits hold the product below)
-  const uint32_t u = (units * t + 15) / 16;
+// Units of a chunk.  It goes by the request's own sizes and the cache's heads alone, so that a request's result is the same bits
+// whatever else the call holds.  t = rows / 64 counts the rows; a chunk takes 2 units and more, as its partial results are written
+// and read, 1 KiB a row, next to 64 KiB of keys and values a unit, and at most 8 t, so that a long context makes more chunks still.
+//   up to 192 rows   about 16 / t chunks of at least 2 t units
+//   more             a KV head has work for many workgroups, and a chunk's own costs are small next to it: 256 / t chunks over all KV
+//                    heads (at least 16 / t a head), of at least t hk / 8 units.  Against the rule above, 32 query heads: one request
+//                    of 64 tokens over 8000 under 4 KV heads 43 us and 109, four 66 and 115, eight 130 and 134, sixteen 239 and 197;
+//                    of 56 tokens under 8 KV heads 45 and 66, 70 and 79, 135 and 123, 258 and 234.  (From 65 rows on: 12 requests of 21
+//                    tokens over 6150, 28 query and 4 KV heads, 90 and 73, one 33 and 45.)
+constexpr uint32_t CACHE_FEW_SPLIT = 16;
+constexpr int32_t cache_many_split(int32_t hk) { return 256 / hk > (int32_t)CACHE_FEW_SPLIT ? 256 / hk : (int32_t)CACHE_FEW_SPLIT; }
+constexpr uint32_t cache_chunk_units(uint32_t units, uint32_t rows, uint32_t hk, uint32_t many_split) {
+  const uint32_t t = rows > 64 ? (rows + 63) / 64 : 1, n = t < 4 ? CACHE_FEW_SPLIT : many_split, most = 8 * t;
+  if (units >= 8 * n) return most;  // (and 32 bits hold the product below)
+  uint32_t least = t < 4 ? 2 * t : t * hk / 8;
+  least = least < 2 ? 2 : least > most ? most : least;
+  const uint32_t u = (units * t + n - 1) / n;
   return u < least ? least : u;
 }
 // Tokens and keys come from device memory: whatever is in it, a share is a share of rows and keys that exist.
 constexpr CacheShare cache_share(int32_t first, int32_t end, int32_t keys, int32_t n_tokens, int32_t most_keys, int32_t group,
-                                 int32_t tile_rows) {
+                                 int32_t tile_rows, int32_t hk, int32_t many_split) {
   if (first < 0) first = 0;
   if (end > n_tokens) end = n_tokens;
   const int32_t fresh = end > first ? end - first : 0;
@@ -97,29 +106,29 @@ constexpr CacheShare cache_share(int32_t first, int32_t end, int32_t keys, int32
   s.rows = fresh * group;  // (32 bits hold n_tokens * group)
   s.tiles = (int32_t)(((uint32_t)s.rows + tile_rows - 1) / (uint32_t)tile_rows);
   s.units = keys > 0 ? (int32_t)(((uint32_t)keys + CACHE_UNIT - 1) / CACHE_UNIT) : 1;
-  const uint32_t u = cache_chunk_units((uint32_t)s.units, (uint32_t)s.rows);
+  const uint32_t u = cache_chunk_units((uint32_t)s.units, (uint32_t)s.rows, (uint32_t)hk, (uint32_t)many_split);
   s.chunks = (int32_t)(((uint32_t)s.units + u - 1) / u);
   return s;
 }
 // Upper bounds of what all requests of a call add up to, per KV head; the kernels' sums never pass them.
 // chunks <= most / t + 1 with t = ceil(rows / 64) and `most` as follows
-constexpr int64_t cache_most_chunks(int64_t most_keys) {
+constexpr int64_t cache_most_chunks(int64_t most_keys, int hk) {
   const int64_t units = (most_keys + CACHE_UNIT - 1) / CACHE_UNIT;
-  return units <= 2 ? 1 : units / 8 > 16 ? (units + 7) / 8 : 16;
+  return units <= 2 ? 1 : units / 8 > cache_many_split(hk) ? (units + 7) / 8 : cache_many_split(hk);
 }
 // rows of partial results: rows * chunks
-constexpr int64_t cache_partial_rows(int64_t n_requests, int64_t n_tokens, int group, int64_t most_keys) {
-  if (cache_most_chunks(most_keys) == 1) return 0;  // no request has two chunks
+constexpr int64_t cache_partial_rows(int64_t n_requests, int64_t n_tokens, int group, int64_t most_keys, int hk) {
+  if (cache_most_chunks(most_keys, hk) == 1) return 0;  // no request has two chunks
   const int64_t rows = n_tokens * group, wide = rows < 64 * n_requests ? rows : 64 * n_requests;
   const int64_t live = n_requests < n_tokens ? n_requests : n_tokens;
-  return wide * cache_most_chunks(most_keys) + rows + 63 * live;
+  return wide * cache_most_chunks(most_keys, hk) + rows + 63 * live;
 }
 // workgroups: tiles * chunks
-constexpr int64_t cache_grid(int64_t n_requests, int64_t n_tokens, int group, int64_t most_keys, int tile_rows) {
+constexpr int64_t cache_grid(int64_t n_requests, int64_t n_tokens, int group, int64_t most_keys, int tile_rows, int hk) {
   const int64_t live = n_requests < n_tokens ? n_requests : n_tokens;
   const int64_t tiles = n_tokens * group / tile_rows + live, per = tile_rows < 64 ? 64 / tile_rows : 1;
   const int64_t wide = tiles < per * live ? tiles : per * live;
-  return wide * cache_most_chunks(most_keys) + tiles;
+  return wide * cache_most_chunks(most_keys, hk) + tiles;
 }
 
 // Place of a workgroup among a request's: `pairs` pairs (chunk, KV head), KV head first, times `tiles`.  Workgroups go round-robin

@@ -51,7 +51,8 @@ def test_shares_stay_inside_their_bounds(tmp_path):
     _run(tmp_path, """
       srand(11);
       for (int round = 0; round < 4000; ++round) {
-        const int group = 1 + rand() % 16, n = 1 + rand() % 9;
+        const int heads[] = {1, 2, 3, 4, 8, 16, 40, 1024};
+        const int group = 1 + rand() % 16, n = 1 + rand() % 9, hk = heads[rand() % 8], split = cache_many_split(hk);
         const int64_t page = 16 << (rand() % 5), most = page * (1 + rand() % (rand() % 2 ? 9000 : 60));
         int64_t start[10] = {0}, keys[9];
         for (int r = 0; r < n; ++r) {
@@ -63,17 +64,17 @@ def test_shares_stay_inside_their_bounds(tmp_path):
         for (int tile : {16, 32, 64, 128, 192}) {
           int64_t rows = 0, items = 0;
           for (int r = 0; r < n; ++r) {
-            const CacheShare s = cache_share(start[r], start[r + 1], keys[r], tokens, most, group, tile);
+            const CacheShare s = cache_share(start[r], start[r + 1], keys[r], tokens, most, group, tile, hk, split);
             if (s.chunks < 1 || s.units < 1 || s.keys > most) return 2;
             const int per = (s.units + s.chunks - 1) / s.chunks;
             if ((int64_t)per * s.chunks < s.units || (int64_t)per * CACHE_UNIT * s.chunks < s.keys) return 3;
-            if (s.tiles && s.chunks > cache_most_chunks(most) / ((s.rows + 63) / 64) + 1) return 4;
-            if (cache_most_chunks(most) == 1 && s.chunks > 1) return 5;
+            if (s.tiles && s.chunks > cache_most_chunks(most, hk) / ((s.rows + 63) / 64) + 1) return 4;
+            if (cache_most_chunks(most, hk) == 1 && s.chunks > 1) return 5;
             if (s.chunks > 1) rows += (int64_t)s.rows * s.chunks;
             items += (int64_t)s.tiles * s.chunks;
           }
-          if (rows > cache_partial_rows(n, tokens, group, most)) { std::printf("rows %lld\\n", (long long)rows); return 6; }
-          if (items > cache_grid(n, tokens, group, most, tile)) { std::printf("items %lld tile %d\\n", (long long)items, tile); return 7; }
+          if (rows > cache_partial_rows(n, tokens, group, most, hk)) { std::printf("rows %lld\\n", (long long)rows); return 6; }
+          if (items > cache_grid(n, tokens, group, most, tile, hk)) { std::printf("items %lld tile %d\\n", (long long)items, tile); return 7; }
         }
       }""")
 
@@ -82,7 +83,7 @@ def test_a_share_of_anything_is_a_share_of_what_exists(tmp_path):
     _run(tmp_path, """
       const int64_t wild[] = {-2147483647 - 1, -1, 0, 1, 7, 100, 2147483647};
       for (int64_t a : wild) for (int64_t b : wild) for (int64_t keys : wild) {
-        const CacheShare s = cache_share(a, b, keys, 50, 4096, 8, 64);
+        const CacheShare s = cache_share(a, b, keys, 50, 4096, 8, 64, 4, cache_many_split(4));
         if (s.first < 0 || s.fresh < 0 || (s.fresh && s.first + s.fresh > 50) || s.keys < 0 || s.keys > 4096) return 1;
         if (s.keys && s.keys < s.fresh) return 2;
       }""")

@@ -284,7 +284,8 @@ def test_attention_of_trees(d, hq, hk, words, news, random_mask):
 
 @pytest.mark.parametrize("d,hq,hk,ctx,new", [
     (128, 4, 1, [2500, 0, 700], [1, 1, 1]), (64, 4, 4, [5000], [2]), (128, 8, 1, [3000, 40], [4, 4]), (64, 16, 2, [1900], [9]),
-    (128, 12, 2, [4100], [17]), (64, 32, 2, [2300, 300], [13, 3])])
+    (128, 12, 2, [4100], [17]), (64, 32, 2, [2300, 300], [13, 3]),
+    (128, 32, 1, [1500, 0, 300], [20, 7, 3]), (64, 16, 2, [2600], [60]), (128, 24, 8, [1700, 90], [64, 2])])
 def test_attention_in_chunks(d, hq, hk, ctx, new):
     """Contexts of several chunks in every kernel, next to short ones, sharp rows among them."""
     words = 0 if max(new) == 1 else 1
