@@ -84,11 +84,12 @@ def _rows(t, shape, strides, device: int, name: str):
 
 # The current stream's handle without a Stream object around it: 0.06 us of a call's 9 instead of 2.5.
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device  # 0.05 us instead of 0.2; a tensor is there
 
 
 def _call(fn, device: int, *args):
     """fn(*args, stream) on the current stream of `device`."""
-    if device == torch.cuda.current_device():
+    if device == _current_device():
         _check(fn(*args, _stream_of(device)))
     else:
         with torch.cuda.device(device):
@@ -205,12 +206,15 @@ def sp_cache_attn(shape: SpStepShape, cache: SpCacheShape, q, k_cache, v_cache, 
 
 def sp_cache_accept(cache: SpCacheShape, k_cache, v_cache, block_table, ctx_len, seq_len, path, n_accepted, ctx_out=None):
     """k_cache, v_cache: [layers][pages][page_size][hkv][d], or one layer's four dimensions; path [requests][max_accept]."""
-    dev, dims = k_cache.get_device(), k_cache.dim()
+    dev, dims, c = k_cache.get_device(), k_cache.dim(), cache
     layers, stride = (1, 0) if dims == 4 else (k_cache.shape[0], k_cache.stride(0))
     (n, width), most = block_table.shape, path.shape[1]
     if v_cache.dim() != dims or dims == 5 and (v_cache.shape[0] != layers or layers > 1 and v_cache.stride(0) != stride):
         raise ValueError("k_cache and v_cache need one geometry")
-    at = [_cache_rows(cache, x if dims == 4 else x[0], dev, name) for x, name in ((k_cache, "k_cache"), (v_cache, "v_cache"))]
+    shape, strides = (c.n_pages, c.page_size, c.n_kv_heads, c.head_dim), (c.stride_page, c.stride_token, c.stride_head, 1)
+    if dims == 5:  # (a layer's view of its own, to look at, would cost a microsecond)
+        shape, strides = (layers, *shape), (stride, *strides)
+    at = _rows(k_cache, shape, strides, dev, "k_cache"), _rows(v_cache, shape, strides, dev, "v_cache")
     _call(lib().sp_cache_accept, dev, ctypes.byref(cache), layers, stride, at[0], at[1], n, width,
           _dev(block_table, _I32, n * width, dev, "block_table"), _dev(ctx_len, _I32, n, dev, "ctx_len"),
           _dev(seq_len, _I32, n, dev, "seq_len"), most, _dev(path, _I32, n * most, dev, "path"),
