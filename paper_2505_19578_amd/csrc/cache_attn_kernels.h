@@ -581,8 +581,9 @@ __device__ __forceinline__ void wait_copies() {
 }
 
 // Steps of 32 keys lie in LDS, four of K and four of V in rings, filled two steps ahead by copies that pass no registers; one
-// barrier for two steps.  A row's 16-byte pieces lie XOR-swizzled by the row number, so that the fragments' reads (16 rows at a time
-// for K, four rows for V) meet no bank twice; the copies' lanes fetch the pieces in that order.
+// barrier for two steps.  A row's 16-byte pieces lie XOR-swizzled by the row number, so that K's fragments (16 rows at a time) meet no
+// bank twice, V's (four rows, two neighbouring pieces of each) no more than twice; the copies' lanes fetch the pieces in that order.
+// (An order in which V's meet none twice either measured the same: LDS is busy a quarter of the time.)
 //
 // Step s: the matrix pipe takes S of step s + 1, then O += V P of step s; beside it the vector unit makes the weights of step s,
 // then the largest of S of step s + 1.
