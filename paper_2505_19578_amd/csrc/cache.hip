@@ -105,11 +105,13 @@ size_t plan_bytes(int32_t n) { return ((size_t)2 * n + 1) * sizeof(int32_t); }
 // ------------------------------------------------------------------------------------------------------------- attention
 // Rows of a workgroup's tile, by the rows (group * max_new) that a request has under one KV head.  Up to 16 the narrow kernel: 64
 // contexts of 8K with 4 rows 412 us and 414 in the wide one, 32 of 3000 with 8 rows 95 and 103, 16 of 500 with 4 16.8 and 18.4
-// (one of 100K 99 and 97).  Two column groups to a wavefront from 65 on: a key's fragment is read from LDS once for 32 rows
-// instead of 16.
+// (one of 100K 99 and 97).  Two column groups to a wavefront, which read a key's fragment from LDS once for 32 rows instead of 16, from
+// 193 rows on: below, shorter steps of more workgroups are faster (us, one group and two: 12 contexts of up to 6150 with 147 rows 42
+// and 52, 8 of 4000 with 128 51 and 51 and with 192 70 and 83, 4 of 30000 with 147 84 and 118), above it turns (4 of 30000 with 224
+// rows 195 and 178, one of 131000 with 512 388 and 330; one of 8000 with 224 31 and 43).
 int attn_tile_rows(const sp_step_shape *s, const sp_cache_shape *c) {
   const int64_t rows = (int64_t)s->max_new * (s->n_q_heads / c->n_kv_heads);
-  return rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
+  return rows <= 16 ? 16 : rows <= 192 ? 64 : 128;
 }
 int64_t attn_most_keys(const sp_step_shape *s, const sp_cache_shape *c) { return (int64_t)s->max_pages * c->page_size; }
 int64_t attn_partial_rows(const sp_step_shape *s, const sp_cache_shape *c) {
@@ -272,7 +274,11 @@ sp_status sp_qk_norm_rope(const sp_rope_shape *shape, const void *q, const void 
     p.page_shift = log2_of(cache->page_size), p.n_slots = (int64_t)cache->n_pages * cache->page_size;
   }
   hipStream_t st = (hipStream_t)hip_stream;
-  const bool four = s.n_tokens >= 2048;
+  // A workgroup takes as many rows at a time as its threads hold.  Where a token's are no multiple of that, long calls take four tokens
+  // to a workgroup (us, one and four, 32768 tokens: 12 rows of 128 of 16 at a time 54 and 39, 36 145 and 130, but 48 173 and 174 and 80
+  // 265 and 280; 2048 tokens of 48 rows of 64 9.1 and 10.0, 4096 14.6 and 13.6)
+  const int rows_of = s.n_q_heads + s.n_kv_heads + (cache ? s.n_kv_heads : 0);
+  const bool four = s.n_tokens >= 4096 && rows_of % (ROPE_THREADS / (s.head_dim / 8)) != 0;
   const dim3 grid((unsigned)(four ? (s.n_tokens + 3) / 4 : s.n_tokens));
   if (s.head_dim == 128 && four)
     hipLaunchKernelGGL((qk_norm_rope_kernel<128, 4>), grid, dim3(ROPE_THREADS), 0, st, p);

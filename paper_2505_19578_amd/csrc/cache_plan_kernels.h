@@ -13,6 +13,10 @@ namespace {
 // of the PLAN_MAX_TREE before them, which is as far as a tree with masks reaches.
 // Bound by latency: a few dependent loads and two scans.  Up to PLAN_ONE_LAUNCH tokens one workgroup does both parts in one
 // launch, with what there is per request kept in LDS; beyond, the second part is spread over the chip.
+// 256 requests of one token 4.3 us, 96 trees of 32 tokens 9.0, 40 prompts of up to 8192 tokens 3.9 and 4.9 (an empty launch: about 2).
+// One launch and two: 256 requests of one token 4.5 us and 6.6, 60 trees of 32 7.4 and 8.6, 4000 tokens of a chain 6.8 and 6.7, and a
+// second launch takes the caller 2.5 us; 120 trees of 32 10.3 and 8.9; from there on one workgroup falls behind (8000 trees' tokens 18.7 and
+// 9.2).
 constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64;
 constexpr int PLAN_ONE_LAUNCH = 4096;           // tokens
 constexpr int PLAN_PART_THREADS = 256;          // and tokens of a workgroup, of the second part's own launch

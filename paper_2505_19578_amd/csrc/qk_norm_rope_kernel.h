@@ -11,7 +11,8 @@ namespace {
 // A workgroup takes TB tokens: it forms the TB * rotary / 2 sines and cosines once, in LDS, and every head of the token uses
 // them.  D / 8 lanes hold a row, four pairs each, as two 8-byte pieces that hold the pairs' halves, so that a pair never
 // crosses lanes whichever way the pairs are laid out.
-// Bound by HBM (each row read once, written once, keys and values twice: output and cache).
+// Bound by HBM (each row read once, written once, keys and values twice: output and cache): 32768 tokens of 32 + 8 heads of 128 172 us
+// = 5.1 TB/s, what a large copy reaches; 1952 tokens 16.7 us = 5.0; one token 4.6 us.
 constexpr int ROPE_THREADS = 256;
 
 struct RopeParams {

@@ -116,7 +116,8 @@ def test_plan_of_nothing_and_chain_masks():
 @pytest.mark.parametrize("tokens,hq,hk,d,rotary,interleaved,norm,cached", [
     (1, 4, 4, 64, 64, False, True, True), (1, 32, 8, 128, 128, False, True, True), (7, 28, 4, 128, 64, True, False, True),
     (33, 1, 1, 64, 8, False, True, False), (130, 64, 8, 128, 128, True, True, True), (5, 6, 2, 64, 32, False, False, True),
-    (2049, 4, 2, 128, 0, False, True, True), (2051, 3, 3, 64, 64, True, True, True), (4097, 2, 1, 128, 120, False, False, False)])
+    (2049, 4, 2, 128, 0, False, True, True), (2051, 3, 3, 64, 64, True, True, True), (4097, 2, 1, 128, 120, False, False, False),
+    (4099, 3, 3, 64, 64, True, True, True), (4096, 12, 2, 128, 128, False, True, True)])
 def test_norm_and_rotation(tokens, hq, hk, d, rotary, interleaved, norm, cached):
     """Against 64 bits: half a bf16 step of the result, and 2^-16 of the pair for the 32-bit arithmetic (a sum of 128 squares,
     2^-17 at most, and a dozen operations of 2^-24)."""
@@ -261,7 +262,7 @@ def _check(s, got, d):
 _CONTEXTS = [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 127, 128, 129, 200]
 
 
-@pytest.mark.parametrize("hq,hk,d,page", [(4, 4, 64, 16), (4, 1, 128, 32), (7, 1, 128, 16), (16, 2, 64, 64), (24, 2, 128, 128), (40, 1, 64, 16)])
+@pytest.mark.parametrize("hq,hk,d,page", [(4, 4, 64, 16), (4, 1, 128, 32), (7, 1, 128, 16), (16, 2, 64, 64), (24, 2, 128, 128), (40, 1, 64, 16), (20, 1, 128, 32)])
 @pytest.mark.parametrize("new", [1, 2, 5, 13])
 def test_attention_at_every_border(hq, hk, d, page, new):
     """Contexts around every border of steps, halves and pages; rows around those of the tiles (group * new = 1 to 520)."""
@@ -306,7 +307,7 @@ def test_attention_of_many_requests(n):
     _check(s, _attend(s), 64)
 
 
-@pytest.mark.parametrize("d,hq,new", [(128, 4, 3), (64, 20, 5), (128, 40, 5)])
+@pytest.mark.parametrize("d,hq,new", [(128, 4, 3), (64, 20, 5), (128, 30, 5), (128, 40, 5)])
 def test_what_a_row_does_not_see_does_not_touch_it(d, hq, new):
     """NaN and infinities in keys and values of other branches, behind the last key, and on pages that nobody holds; infinite
     and NaN values that a row does see come out as the sum says."""
@@ -348,7 +349,7 @@ def test_what_a_row_does_not_see_does_not_touch_it(d, hq, new):
                     assert np.array_equal(got[0][t], want[0][t]) and np.array_equal(got[1][t], want[1][t]), (r, t)
 
 
-@pytest.mark.parametrize("new", [1, 9, 40])
+@pytest.mark.parametrize("new", [1, 9, 40, 60])
 def test_pages_that_do_not_exist_hold_no_keys(new):
     s = _step([100, 40, 0, 700], [new] * 4, 4, 1, 128, 16, 0 if new == 1 else 1, new)
     s["table"][0, 2] = -1
@@ -441,6 +442,17 @@ def test_a_request_does_not_depend_on_its_company():
         one = dict(s, q=s["q"][a:b], table=s["table"][r:r + 1], seq=s["seq"][r:r + 1], start=np.array([0, b - a]), mask=s["mask"][a:b])
         got = _attend(one)
         assert np.array_equal(got[0], both[0][a:b]) and np.array_equal(got[1], both[1][a:b]), r
+
+
+@pytest.mark.parametrize("d,hq,hk", [(128, 8, 2), (64, 6, 2)])
+def test_the_tile_does_not_change_a_result(d, hq, hk):
+    """The two tiles for many rows give the same bits, whichever of them max_new selects; more new tokens than max_new says are
+    right as well."""
+    s = _step([700, 33, 3000, 0], [20, 9, 3, 13], hq, hk, d, 16, 0, 78)
+    a, b, c = _attend(s), _attend(s, top=100), _attend(s, top=6)
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1]) and np.array_equal(a[0], c[0]) and np.array_equal(a[1], c[1])
+    _check(s, b, d)
+    _check(s, _attend(s, top=1), d)
 
 
 def test_offsets_that_pass_32_bits():
