@@ -220,9 +220,11 @@ sp_status sp_cache_plan(int32_t n_requests, int32_t max_tokens, int32_t page_siz
   p.n = n_requests, p.max_tokens = max_tokens, p.page_shift = log2_of(page_size), p.width = max_pages, p.words = mask_words;
   p.free_capacity = free_capacity;
   hipStream_t st = (hipStream_t)hip_stream;
-  const bool one = max_tokens <= PLAN_ONE_LAUNCH;
-  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, p, one ? 1 : 0);
-  if ((rc = launched("plan_kernel")) || one) return rc;
+  const bool spread = n_requests <= PLAN_THREADS && n_held_out != n_held && n_free_out != n_free;
+  const bool one = !spread && max_tokens <= PLAN_ONE_LAUNCH;
+  const unsigned groups = spread ? (unsigned)std::max((max_tokens + PLAN_THREADS - 1) / PLAN_THREADS, 1) : 1;
+  hipLaunchKernelGGL(plan_kernel, dim3(groups), dim3(PLAN_THREADS), 0, st, p, spread ? PLAN_THREADS : one ? PLAN_ONE_LAUNCH : 0);
+  if ((rc = launched("plan_kernel")) || spread || one) return rc;
   hipLaunchKernelGGL(plan_tokens_kernel, dim3((unsigned)((max_tokens + PLAN_PART_THREADS - 1) / PLAN_PART_THREADS)), dim3(PLAN_PART_THREADS),
                      0, st, p);
   return launched("plan_tokens_kernel");

@@ -11,12 +11,16 @@ namespace {
 // Page entries that are read are those the request held before, the ones that are written come after them, so tokens need no
 // order among each other.  A token's ancestors are walked up from it, in LDS, where a workgroup lays the parents of its tokens and
 // of the PLAN_MAX_TREE before them, which is as far as a tree with masks reaches.
-// Bound by latency: a few dependent loads and two scans.  Up to PLAN_ONE_LAUNCH tokens one workgroup does both parts in one
-// launch, with what there is per request kept in LDS; beyond, the second part is spread over the chip.
-// 256 requests of one token 4.3 us, 96 trees of 32 tokens 9.0, 40 prompts of up to 8192 tokens 3.9 and 4.9 (an empty launch: about 2).
-// One launch and two: 256 requests of one token 4.5 us and 6.6, 60 trees of 32 7.4 and 8.6, 4000 tokens of a chain 6.8 and 6.7, and a
-// second launch takes the caller 2.5 us; 120 trees of 32 10.3 and 8.9; from there on one workgroup falls behind (8000 trees' tokens 18.7 and
-// 9.2).
+// Bound by latency: a few dependent loads and two scans; 256 requests of one token 4.3 us (an empty launch: about 2).  Three ways:
+//   spread       up to PLAN_THREADS requests: every workgroup does the first part for itself, in LDS, and PLAN_THREADS tokens of the
+//                second; the first one writes what there is per request.  One launch of any number of tokens, but what the first
+//                part reads may not be what it writes: not for n_held and n_free that are updated in place.
+//   one          otherwise, up to PLAN_ONE_LAUNCH tokens: one workgroup does both parts
+//   two launches otherwise: the second part is spread over the chip.
+// Spread and what it would be otherwise (us on the device; a second launch takes its caller 2.5 more): 256 requests of one token 4.7 and
+// 4.5, 96 trees of 32 tokens 5.9 and 9.4, 250 6.0 and 9.4, 4000 tokens of chains 4.7 and 6.8, 1000 requests of 8 tokens 5.5 and 9.4, 40
+// of 8192 8.8 and 8.3, 400 trees of 256 16.2 and 14.8.  One and two launches: 256 requests of one token 4.5 and 6.6, 60 trees of 32
+// 7.4 and 8.6, 120 10.3 and 8.9, 8000 trees' tokens 18.7 and 9.2.
 constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64;
 constexpr int PLAN_ONE_LAUNCH = 4096;           // tokens
 constexpr int PLAN_PART_THREADS = 256;          // and tokens of a workgroup, of the second part's own launch
@@ -51,9 +55,10 @@ __device__ __forceinline__ uint64_t block_scan(uint64_t x, uint64_t *room, uint6
   return x + (w > 0 ? at(uniform(w) - 1) : 0);
 }
 
-// Keep: called with (request, start of the next one, PlanRequest) for every request
+// Keep: called with (request, start of the next one, PlanRequest) for every request.  lead: this workgroup writes the outputs.
+// Returns the number of free pages before the call.
 template <class Keep>
-__device__ __forceinline__ void plan_requests(const PlanParams &p, uint64_t (&room)[4][PLAN_WAVES], Keep &&keep) {
+__device__ __forceinline__ int plan_requests(const PlanParams &p, bool lead, uint64_t (&room)[4][PLAN_WAVES], Keep &&keep) {
   uint64_t tokens = 0, pages = 0;  // before this round's requests
   int n_free = p.n_free[0];
   n_free = n_free < 0 ? 0 : n_free > p.free_capacity ? p.free_capacity : n_free;
@@ -70,24 +75,27 @@ __device__ __forceinline__ void plan_requests(const PlanParams &p, uint64_t (&ro
     const uint64_t lack = live && st == PLAN_OK ? plan_lacking((int64_t)ctx + fresh, held, 1 << p.page_shift) : 0;
     const uint64_t last = pages + block_scan(lack, room[2 * round + 1], total);
     // the first request for which the pages do not suffice knows how many were given out: all those before it
-    if (lack > 0 && last > (uint64_t)n_free && last - lack <= (uint64_t)n_free) p.n_free_out[0] = n_free - (int)(last - lack);
+    if (lead && lack > 0 && last > (uint64_t)n_free && last - lack <= (uint64_t)n_free) p.n_free_out[0] = n_free - (int)(last - lack);
     pages += total;
     if (st == PLAN_OK && lack > 0 && last > (uint64_t)n_free) st = PLAN_NO_PAGES;
     const bool ok = st == PLAN_OK;
     if (live) {
       const int start = (int)(end < (uint64_t)p.max_tokens ? end : p.max_tokens);
-      p.tok_start[r + 1] = start;
-      p.seq_len[r] = ok ? ctx + fresh : 0;
-      p.status[r] = st;
-      p.held_out[r] = ok ? held + (int)lack : held;
+      if (lead) {
+        p.tok_start[r + 1] = start;
+        p.seq_len[r] = ok ? ctx + fresh : 0;
+        p.status[r] = st;
+        p.held_out[r] = ok ? held + (int)lack : held;
+      }
       keep(r, start, PlanRequest{ctx, held, ok ? (int)(last - lack) : -1, 0});
     }
   }
-  if (threadIdx.x == 0) {
+  if (lead && threadIdx.x == 0) {
     p.tok_start[0] = 0;
     p.free_count[0] = n_free;
     if (pages <= (uint64_t)n_free) p.n_free_out[0] = n_free - (int)pages;
   }
+  return n_free;
 }
 
 // Tokens t0 + threadIdx, + threads, .. below t1.  start(r) and request(r): of the requests; up: parents of tokens up0 .. in LDS.
@@ -165,32 +173,35 @@ __device__ __forceinline__ void plan_tokens(const PlanParams &p, int n_free, int
 // parents as they are laid in LDS: what no tree with masks can hold is no parent
 __device__ __forceinline__ int16_t short_parent(int x) { return x < 0 || x >= PLAN_MAX_TREE ? -1 : (int16_t)x; }
 
-__global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(PlanParams p, int with_tokens) {
+// each: tokens of a workgroup, at most PLAN_ONE_LAUNCH; 0: the tokens are another launch's
+__global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(PlanParams p, int each) {
   __shared__ uint64_t room[4][PLAN_WAVES];
-  __shared__ int16_t up[PLAN_ONE_LAUNCH];
+  __shared__ int16_t up[PLAN_MAX_TREE + PLAN_ONE_LAUNCH];
   __shared__ int32_t starts[PLAN_THREADS + 1];
   __shared__ PlanRequest requests[PLAN_THREADS];
   const int tid = threadIdx.x;
-  if (with_tokens && p.parents && p.words)
-    for (int t = tid; t < p.max_tokens; t += PLAN_THREADS) up[t] = short_parent(p.parents[t]);
+  const bool lead = blockIdx.x == 0;
+  const int t0 = (int)blockIdx.x * each, t1 = min(p.max_tokens, t0 + each), up0 = max(0, t0 - PLAN_MAX_TREE);
+  if (each && p.parents && p.words)
+    for (int t = up0 + tid; t < t1; t += PLAN_THREADS) up[t - up0] = short_parent(p.parents[t]);
   if (tid == 0) starts[0] = 0;
-  if (with_tokens && p.n <= PLAN_THREADS) {
-    plan_requests(p, room, [&](int r, int start, const PlanRequest &q) {
+  if (each && p.n <= PLAN_THREADS) {
+    const int n_free = plan_requests(p, lead, room, [&](int r, int start, const PlanRequest &q) {
       starts[r + 1] = start;
       requests[r] = q;
     });
     __syncthreads();
-    plan_tokens(p, p.free_count[0], 0, p.max_tokens, PLAN_THREADS, [&](int r) { return starts[r]; }, [&](int r) { return requests[r]; }, up, 0);
+    plan_tokens(p, n_free, t0, t1, PLAN_THREADS, [&](int r) { return starts[r]; }, [&](int r) { return requests[r]; }, up, up0);
     return;
   }
-  plan_requests(p, room, [&](int r, int, const PlanRequest &q) {
+  const int n_free = plan_requests(p, lead, room, [&](int r, int, const PlanRequest &q) {
     p.old_held[r] = q.held;
     p.page_start[r] = q.page_start;
   });
-  if (!with_tokens) return;
+  if (!each) return;
   __syncthreads();
-  plan_tokens(p, p.free_count[0], 0, p.max_tokens, PLAN_THREADS, [&](int r) { return p.tok_start[r]; },
-              [&](int r) { return PlanRequest{p.ctx[r], p.old_held[r], p.page_start[r], 0}; }, up, 0);
+  plan_tokens(p, n_free, t0, t1, PLAN_THREADS, [&](int r) { return p.tok_start[r]; },
+              [&](int r) { return PlanRequest{p.ctx[r], p.old_held[r], p.page_start[r], 0}; }, up, up0);
 }
 
 __global__ __launch_bounds__(PLAN_PART_THREADS) void plan_tokens_kernel(PlanParams p) {
