@@ -163,7 +163,7 @@ sp_status launch_cache_attn(const CacheAttnParams &p, int tile_rows, int64_t ite
   else
     hipLaunchKernelGGL((cache_attn_wide_kernel<D, 2>), grid, block, 0, st, p);
   const sp_status rc = launched("cache_attn_kernel");
-  if (rc || cache_most_chunks(p.most_keys, p.hk) == 1) return rc;  // no request has two chunks
+  if (rc || !cache_any_chunks(p.most_keys)) return rc;  // no request has two chunks
   const int64_t rows = (int64_t)p.n_tok * p.hq;
   hipLaunchKernelGGL((cache_join_kernel<D>), dim3((unsigned)std::min((rows + CA_WAVES - 1) / CA_WAVES, CA_GRID)), block, 0, st, p);
   return launched("cache_join_kernel");

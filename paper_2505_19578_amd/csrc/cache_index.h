@@ -111,24 +111,29 @@ constexpr CacheShare cache_share(int32_t first, int32_t end, int32_t keys, int32
   return s;
 }
 // Upper bounds of what all requests of a call add up to, per KV head; the kernels' sums never pass them.
-// chunks <= most / t + 1 with t = ceil(rows / 64) and `most` as follows
-constexpr int64_t cache_most_chunks(int64_t most_keys, int hk) {
+// chunks <= most / t + 1 with t = ceil(rows / 64) and `most` as follows; from 193 rows on with the larger split
+constexpr int64_t cache_most_chunks(int64_t most_keys, int64_t split) {
   const int64_t units = (most_keys + CACHE_UNIT - 1) / CACHE_UNIT;
-  return units <= 2 ? 1 : units / 8 > cache_many_split(hk) ? (units + 7) / 8 : cache_many_split(hk);
+  return units <= 2 ? 1 : (units + 7) / 8 > split ? (units + 7) / 8 : split;
+}
+constexpr bool cache_any_chunks(int64_t most_keys) { return cache_most_chunks(most_keys, CACHE_FEW_SPLIT) > 1; }
+// what the requests of 193 rows and more add to a bound with the smaller split: how many there can be, times the difference
+constexpr int64_t cache_many_extra(int64_t n_requests, int64_t rows, int64_t most_keys, int hk) {
+  const int64_t many = rows / 193 < n_requests ? rows / 193 : n_requests;
+  return many * (cache_most_chunks(most_keys, cache_many_split(hk)) - cache_most_chunks(most_keys, CACHE_FEW_SPLIT));
 }
 // rows of partial results: rows * chunks
 constexpr int64_t cache_partial_rows(int64_t n_requests, int64_t n_tokens, int group, int64_t most_keys, int hk) {
-  if (cache_most_chunks(most_keys, hk) == 1) return 0;  // no request has two chunks
+  if (!cache_any_chunks(most_keys)) return 0;
   const int64_t rows = n_tokens * group, wide = rows < 64 * n_requests ? rows : 64 * n_requests;
-  const int64_t live = n_requests < n_tokens ? n_requests : n_tokens;
-  return wide * cache_most_chunks(most_keys, hk) + rows + 63 * live;
+  return wide * cache_most_chunks(most_keys, CACHE_FEW_SPLIT) + 64 * cache_many_extra(n_requests, rows, most_keys, hk) + rows;
 }
 // workgroups: tiles * chunks
 constexpr int64_t cache_grid(int64_t n_requests, int64_t n_tokens, int group, int64_t most_keys, int tile_rows, int hk) {
-  const int64_t live = n_requests < n_tokens ? n_requests : n_tokens;
-  const int64_t tiles = n_tokens * group / tile_rows + live, per = tile_rows < 64 ? 64 / tile_rows : 1;
+  const int64_t live = n_requests < n_tokens ? n_requests : n_tokens, rows = n_tokens * group;
+  const int64_t tiles = rows / tile_rows + live, per = tile_rows < 64 ? 64 / tile_rows : 1;
   const int64_t wide = tiles < per * live ? tiles : per * live;
-  return wide * cache_most_chunks(most_keys, hk) + tiles;
+  return wide * cache_most_chunks(most_keys, CACHE_FEW_SPLIT) + per * cache_many_extra(n_requests, rows, most_keys, hk) + tiles;
 }
 
 // Place of a workgroup among a request's: `pairs` pairs (chunk, KV head), KV head first, times `tiles`.  Workgroups go round-robin

@@ -50,13 +50,13 @@ def test_shares_stay_inside_their_bounds(tmp_path):
     sized for, whatever the lengths are."""
     _run(tmp_path, """
       srand(11);
-      for (int round = 0; round < 4000; ++round) {
+      for (int round = 0; round < 20000; ++round) {
         const int heads[] = {1, 2, 3, 4, 8, 16, 40, 1024};
         const int group = 1 + rand() % 16, n = 1 + rand() % 9, hk = heads[rand() % 8], split = cache_many_split(hk);
         const int64_t page = 16 << (rand() % 5), most = page * (1 + rand() % (rand() % 2 ? 9000 : 60));
         int64_t start[10] = {0}, keys[9];
         for (int r = 0; r < n; ++r) {
-          start[r + 1] = start[r] + (rand() % 3 ? rand() % 5 : rand() % 300);
+          start[r + 1] = start[r] + (round % 4 == 0 ? (193 + rand() % 70) / group : rand() % 3 ? rand() % 5 : rand() % 300);
           keys[r] = rand() % 7 ? (int64_t)rand() % (most + 1) : most;
         }
         const int64_t tokens = start[n];
@@ -68,8 +68,8 @@ def test_shares_stay_inside_their_bounds(tmp_path):
             if (s.chunks < 1 || s.units < 1 || s.keys > most) return 2;
             const int per = (s.units + s.chunks - 1) / s.chunks;
             if ((int64_t)per * s.chunks < s.units || (int64_t)per * CACHE_UNIT * s.chunks < s.keys) return 3;
-            if (s.tiles && s.chunks > cache_most_chunks(most, hk) / ((s.rows + 63) / 64) + 1) return 4;
-            if (cache_most_chunks(most, hk) == 1 && s.chunks > 1) return 5;
+            if (s.tiles && s.chunks > cache_most_chunks(most, s.rows < 193 ? CACHE_FEW_SPLIT : split) / ((s.rows + 63) / 64) + 1) return 4;
+            if (!cache_any_chunks(most) && s.chunks > 1) return 5;
             if (s.chunks > 1) rows += (int64_t)s.rows * s.chunks;
             items += (int64_t)s.tiles * s.chunks;
           }
