@@ -73,10 +73,10 @@ def _requests(rng, n, page, width, most_new, bad):
     return ctx, new, held, table
 
 
-# one launch and two (above 4096 tokens), one round of requests and several (above 1024)
+# one workgroup and several (above 1024 tokens; in place: two launches above 4096), one round of requests and several (above 1024)
 @pytest.mark.parametrize("n,page,width,most_new,tree", [
     (1, 16, 1, 16, 0), (1, 16, 8, 1, 0), (3, 16, 5, 40, 0), (64, 32, 20, 3, 1), (37, 64, 6, 64, 1), (20, 16, 40, 256, 4), (19, 128, 9, 200, 4),
-    (1025, 16, 4, 1, 0), (2500, 32, 3, 5, 1), (40, 64, 200, 9000, 0), (70, 16, 40, 128, 2), (300, 16, 30, 40, 1)])
+    (1025, 16, 4, 1, 0), (1024, 16, 9, 9, 1), (2500, 32, 3, 5, 1), (40, 64, 200, 9000, 0), (70, 16, 40, 128, 2), (300, 16, 30, 40, 1)])
 @pytest.mark.parametrize("bad", [False, True])
 def test_plan(n, page, width, most_new, tree, bad):
     from oracle import cache as oracle
@@ -295,6 +295,13 @@ def test_attention_in_chunks(d, hq, hk, ctx, new):
     _check(s, _attend(s), d)
     o, _ = _attend(s, lse=False)
     assert np.array_equal(o, _attend(s)[0])
+
+
+@pytest.mark.parametrize("hq,hk", [(1024, 1), (1024, 1024), (1024, 128)])
+def test_attention_of_the_most_heads(hq, hk):
+    s = _step([300, 0, 17], [2, 1, 0], hq, hk, 64, 16, 1, hq + hk)
+    print(f"[attn] {hq}/{hk}", flush=True)
+    _check(s, _attend(s), 64)
 
 
 @pytest.mark.parametrize("n", [64, 65, 130, 200])
