@@ -282,14 +282,22 @@ sp_status sp_qk_norm_rope(const sp_rope_shape *shape, const void *q, const void 
   const int rows_of = s.n_q_heads + s.n_kv_heads + (cache ? s.n_kv_heads : 0);
   const bool four = s.n_tokens >= 4096 && rows_of % (ROPE_THREADS / (s.head_dim / 8)) != 0;
   const dim3 grid((unsigned)(four ? (s.n_tokens + 3) / 4 : s.n_tokens));
-  if (s.head_dim == 128 && four)
-    hipLaunchKernelGGL((qk_norm_rope_kernel<128, 4>), grid, dim3(ROPE_THREADS), 0, st, p);
-  else if (s.head_dim == 128)
-    hipLaunchKernelGGL((qk_norm_rope_kernel<128, 1>), grid, dim3(ROPE_THREADS), 0, st, p);
-  else if (four)
-    hipLaunchKernelGGL((qk_norm_rope_kernel<64, 4>), grid, dim3(ROPE_THREADS), 0, st, p);
+  const bool whole = s.rotary_dim == s.head_dim;
+  auto launch = [&](auto d, auto tokens) {
+    constexpr int D = decltype(d)::value, TB = decltype(tokens)::value;
+    if (whole)
+      hipLaunchKernelGGL((qk_norm_rope_kernel<D, TB, true>), grid, dim3(ROPE_THREADS), 0, st, p);
+    else
+      hipLaunchKernelGGL((qk_norm_rope_kernel<D, TB, false>), grid, dim3(ROPE_THREADS), 0, st, p);
+  };
+  constexpr std::integral_constant<int, 128> d128{};
+  constexpr std::integral_constant<int, 64> d64{};
+  constexpr std::integral_constant<int, 4> t4{};
+  constexpr std::integral_constant<int, 1> t1{};
+  if (s.head_dim == 128)
+    four ? launch(d128, t4) : launch(d128, t1);
   else
-    hipLaunchKernelGGL((qk_norm_rope_kernel<64, 1>), grid, dim3(ROPE_THREADS), 0, st, p);
+    four ? launch(d64, t4) : launch(d64, t1);
   return launched("qk_norm_rope_kernel");
 }
 

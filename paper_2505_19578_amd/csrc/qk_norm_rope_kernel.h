@@ -11,6 +11,9 @@ namespace {
 // A workgroup takes TB tokens: it forms the TB * rotary / 2 sines and cosines once, in LDS, and every head of the token uses
 // them.  D / 8 lanes hold a row, four pairs each, as two 8-byte pieces that hold the pairs' halves, so that a pair never
 // crosses lanes whichever way the pairs are laid out.
+// WHOLE: every element of a head is rotated (rotary == D).  Otherwise (rotary is a multiple of 8) a lane's four pairs are all
+// rotated or none is, and elements that are not keep their value: the turn (1, 0) would give them 0 times a partner that may be
+// infinite.  Of its own, as the eight choices cost 1.5 % of a long prompt whose heads are rotated whole (176 us and 173).
 // Bound by HBM (each row read once, written once, keys and values twice: output and cache): 32768 tokens of 32 + 8 heads of 128 172 us
 // = 5.1 TB/s, what a large copy reaches; 1952 tokens 16.7 us = 5.0; one token 4.6 us.
 constexpr int ROPE_THREADS = 256;
@@ -41,7 +44,7 @@ __device__ __forceinline__ void rope_pieces(int j, int rotary, int interleaved, 
   }
 }
 
-template <int D, int TB>
+template <int D, int TB, bool WHOLE>
 __global__ __launch_bounds__(ROPE_THREADS) void qk_norm_rope_kernel(RopeParams p) {
   constexpr int L = D / 8, GROUPS = ROPE_THREADS / L;  // lanes of a row, rows at a time
   __shared__ float2 turn[TB][D / 2];                   // cos, sin of a token's pairs; (1, 0) where nothing is rotated
@@ -58,6 +61,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void qk_norm_rope_kernel(RopeParams p
     turn[t][pair] = cs;
   }
   __syncthreads();
+  const bool turned = WHOLE || 8 * j < p.rotary;
   int a, b;
   rope_pieces<D>(j, p.rotary, p.interleaved, a, b);
   float wq[8], wk[8];
@@ -119,6 +123,10 @@ __global__ __launch_bounds__(ROPE_THREADS) void qk_norm_rope_kernel(RopeParams p
         y[e] = f[e] * cs[e].x - f[e + 4] * cs[e].y;
         y[e + 4] = f[e] * cs[e].y + f[e + 4] * cs[e].x;
       }
+    }
+    if (!WHOLE && !turned) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = f[e];
     }
     const u32x2 ya = {pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])}, yb = {pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
     uint16_t *dst = is_q ? p.q_out + (int64_t)tok * p.qo_st + (int64_t)h * p.qo_sh
