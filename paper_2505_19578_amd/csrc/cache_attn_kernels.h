@@ -303,9 +303,11 @@ struct CacheRows {
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; ++d) {
+        const u32x4 bits = __builtin_bit_cast(u32x4, o[c][d]);  // (of a vector's element the compiler takes the first one's bits)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) high = max(high, __builtin_bit_cast(uint32_t, o[c][d][r]) & 0x7fffffffu);
+        for (int r = 0; r < 4; ++r) high = max(high, bits[r] & 0x7fffffffu);
+      }
     return any_lane(high >= 0x7f800000u);
   }
   // row sums over the lanes that share a column
