@@ -22,6 +22,7 @@ namespace {
 // a request do not depend on what else the call holds.
 constexpr int CA_THREADS = 256, CA_WAVES = 4;
 constexpr float CA_SLACK = 8.0f;  // how far (log2) a row's maximum may outgrow its reference before the reference moves
+constexpr float CA_LEAST = 1.17549435e-38f;  // 2^-126: what stands for a factor that 32 bits do not hold, where O is infinite
 constexpr float CA_NONE = -3.0e38f;  // the reference of a row that has seen nothing: finite, so that 2^(-infinity - it) is 0
 
 struct CacheAttnParams {
@@ -167,6 +168,9 @@ struct CacheRows {
   f32x4 o[NC][DT], ones[NC];
   // reference (log2), what a product has to exceed to move it, sum of the weights
   float m[NC], limit[NC], l[NC];
+  // CA_LEAST where this lane's part of O got something infinite: O's factors, 2^(difference of references), are no less than that, as
+  // 0 times an infinite element would be NaN, and it is not to be left out either.  (0 in all other rows: their bits do not change.)
+  float least[NC];
   int tok[NC];  // the column's new token
 
   __device__ __forceinline__ void begin(const CacheAttnParams &p, const CacheRequest &rq, int kvh, int row0, int g, int i) {
@@ -194,6 +198,7 @@ struct CacheRows {
       m[c] = CA_NONE;
       limit[c] = -INFINITY;
       l[c] = 0.f;
+      least[c] = 0.f;
     }
   }
   // Bits of the step's keys that column c's query sees, from key 4 g of each half on (bits 0 .. 3 and 16 .. 19).  mask: the words of
@@ -230,8 +235,9 @@ struct CacheRows {
         limit[c] = t + CA_SLACK / scale;
         l[c] *= f;
         ones[c] *= f;
+        const float fo = fmaxf(f, least[c]);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[c][d] *= f;
+        for (int d = 0; d < DT; ++d) o[c][d] *= fo;
       }
     }
   }
@@ -294,7 +300,7 @@ struct CacheRows {
         const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, seen[c], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (n[r] > 0.f) o[c][d][r] += value_of_kind(kind);
+          if (n[r] > 0.f) o[c][d][r] += value_of_kind(kind), least[c] = CA_LEAST;
       }
     }
   }
@@ -515,10 +521,9 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_narrow_kernel(CacheA
         float top = sm[0][16 * c + i];
 #pragma unroll
         for (int x = 1; x < CA_WAVES; ++x) top = fmaxf(top, sm[x][16 * c + i]);
-        const float f = rows.m[c] == CA_NONE ? 0.f : __builtin_amdgcn_exp2f(rows.m[c] - top);
+        const float f = fmaxf(rows.m[c] == CA_NONE ? 0.f : __builtin_amdgcn_exp2f(rows.m[c] - top), rows.least[c]);
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-          *(f32x4 *)(sum + (w * 16 + i) * OROW + 16 * d + 4 * g) = f == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : rows.o[c][d] * f;
+        for (int d = 0; d < DT; ++d) *(f32x4 *)(sum + (w * 16 + i) * OROW + 16 * d + 4 * g) = rows.o[c][d] * f;
       }
       __syncthreads();
       const int row = it.tile * ROWS + 16 * c + orow;
@@ -942,6 +947,17 @@ __global__ __launch_bounds__(CA_THREADS) void cache_join_kernel(CacheAttnParams 
           if (c + a < n && fc != 0.f)
 #pragma unroll
             for (int e = 0; e < E; ++e) y[e] += fc * z[a][e];
+        }
+      }
+      // a chunk whose factor 32 bits do not hold still gives what is not finite in it
+      uint64_t far = __builtin_amdgcn_ballot_w64(f == 0.f && ml[0] != CA_NONE);
+      while (__builtin_expect(far != 0, 0)) {
+        const int c = c0 + __builtin_ctzll(far);
+        far &= far - 1;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float x = p.part_o[(from + c) * D + E * lane + e];
+          if ((__builtin_bit_cast(uint32_t, x) & 0x7f800000u) == 0x7f800000u) y[e] += x;
         }
       }
     }
