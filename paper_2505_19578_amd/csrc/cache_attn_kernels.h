@@ -120,9 +120,8 @@ __device__ __forceinline__ CacheItem item_of(const CacheRequest &rq, int index, 
   it.chunk = (int)((uint32_t)place.pair / (uint32_t)hk);
   it.kvh = place.pair - it.chunk * hk;
   it.tile = place.tile;
-  const int per = (int)((uint32_t)(rq.s.units + rq.s.chunks - 1) / (uint32_t)rq.s.chunks);
-  it.k_begin = it.chunk * per * CACHE_UNIT;
-  it.k_end = min(rq.s.keys, it.k_begin + per * CACHE_UNIT);
+  const CacheKeys keys = cache_chunk_keys(rq.s, it.chunk);
+  it.k_begin = keys.begin, it.k_end = keys.end;
   it.ctx = rq.s.keys - rq.s.fresh;
   return it;
 }

@@ -87,7 +87,8 @@ constexpr uint32_t CACHE_FEW_SPLIT = 16;
 constexpr int32_t cache_many_split(int32_t hk) { return 256 / hk > (int32_t)CACHE_FEW_SPLIT ? 256 / hk : (int32_t)CACHE_FEW_SPLIT; }
 constexpr uint32_t cache_chunk_units(uint32_t units, uint32_t rows, uint32_t hk, uint32_t many_split) {
   const uint32_t t = rows > 64 ? (rows + 63) / 64 : 1, n = t < 4 ? CACHE_FEW_SPLIT : many_split, most = 8 * t;
-  if (units >= 8 * n) return most;  // (and 32 bits hold the product below)
+  // (32 bits hold the product below up to t = 2^21; from there on `least` exceeds the units, of which there are fewer than 2048: one chunk)
+  if (units >= 8 * n) return most;
   uint32_t least = t < 4 ? 2 * t : t * hk / 8;
   least = least < 2 ? 2 : least > most ? most : least;
   const uint32_t u = (units * t + n - 1) / n;
@@ -109,6 +110,15 @@ constexpr CacheShare cache_share(int32_t first, int32_t end, int32_t keys, int32
   const uint32_t u = cache_chunk_units((uint32_t)s.units, (uint32_t)s.rows, (uint32_t)hk, (uint32_t)many_split);
   s.chunks = (int32_t)(((uint32_t)s.units + u - 1) / u);
   return s;
+}
+// Keys of a chunk: as many units for each, and the last one ends with the request.
+struct CacheKeys {
+  int32_t begin, end;
+};
+constexpr CacheKeys cache_chunk_keys(const CacheShare &s, int32_t chunk) {
+  const int32_t per = (int32_t)((uint32_t)(s.units + s.chunks - 1) / (uint32_t)s.chunks);
+  const int32_t begin = chunk * per * CACHE_UNIT, left = s.keys - begin;  // (the last chunk's units may end behind what 32 bits number)
+  return CacheKeys{begin, begin + (left < per * CACHE_UNIT ? left : per * CACHE_UNIT)};
 }
 // Upper bounds of what all requests of a call add up to, per KV head; the kernels' sums never pass them.
 // chunks <= most / t + 1 with t = ceil(rows / 64) and `most` as follows; from 193 rows on with the larger split
