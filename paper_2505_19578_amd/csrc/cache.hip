@@ -281,24 +281,26 @@ sp_status sp_qk_norm_rope(const sp_rope_shape *shape, const void *q, const void 
   // 265 and 280; 2048 tokens of 48 rows of 64 9.1 and 10.0, 4096 14.6 and 13.6)
   const int rows_of = s.n_q_heads + s.n_kv_heads + (cache ? s.n_kv_heads : 0);
   const bool four = s.n_tokens >= 4096 && rows_of % (ROPE_THREADS / (s.head_dim / 8)) != 0;
-  const dim3 grid((unsigned)(four ? (s.n_tokens + 3) / 4 : s.n_tokens));
   const bool whole = s.rotary_dim == s.head_dim;
-  auto launch = [&](auto d, auto tokens) {
+  auto launch = [&](auto d, auto tokens) -> sp_status {
     constexpr int D = decltype(d)::value, TB = decltype(tokens)::value;
-    if (whole)
-      hipLaunchKernelGGL((qk_norm_rope_kernel<D, TB, true>), grid, dim3(ROPE_THREADS), 0, st, p);
-    else
-      hipLaunchKernelGGL((qk_norm_rope_kernel<D, TB, false>), grid, dim3(ROPE_THREADS), 0, st, p);
+    static_assert(ROPE_LAUNCH % TB == 0 && (int64_t)ROPE_LAUNCH / TB * ROPE_THREADS < (1ll << 32), "a launch's threads");
+    for (; p.first < p.tokens; p.first += ROPE_LAUNCH) {  // (2^28 + 2^22 at most)
+      const dim3 grid((unsigned)((std::min(p.tokens - p.first, ROPE_LAUNCH) + TB - 1) / TB));
+      if (whole)
+        hipLaunchKernelGGL((qk_norm_rope_kernel<D, TB, true>), grid, dim3(ROPE_THREADS), 0, st, p);
+      else
+        hipLaunchKernelGGL((qk_norm_rope_kernel<D, TB, false>), grid, dim3(ROPE_THREADS), 0, st, p);
+      if (const sp_status e = launched("qk_norm_rope_kernel")) return e;
+    }
+    return SP_OK;
   };
   constexpr std::integral_constant<int, 128> d128{};
   constexpr std::integral_constant<int, 64> d64{};
   constexpr std::integral_constant<int, 4> t4{};
   constexpr std::integral_constant<int, 1> t1{};
-  if (s.head_dim == 128)
-    four ? launch(d128, t4) : launch(d128, t1);
-  else
-    four ? launch(d64, t4) : launch(d64, t1);
-  return launched("qk_norm_rope_kernel");
+  if (s.head_dim == 128) return four ? launch(d128, t4) : launch(d128, t1);
+  return four ? launch(d64, t4) : launch(d64, t1);
 }
 
 sp_status sp_cache_attn_workspace_bytes(const sp_step_shape *shape, const sp_cache_shape *cache, size_t *bytes) {

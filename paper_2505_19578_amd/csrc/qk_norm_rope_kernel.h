@@ -17,6 +17,7 @@ namespace {
 // Bound by HBM (each row read once, written once, keys and values twice: output and cache): 32768 tokens of 32 + 8 heads of 128 172 us
 // = 5.1 TB/s, what a large copy reaches; 1952 tokens 16.7 us = 5.0; one token 4.6 us.
 constexpr int ROPE_THREADS = 256;
+constexpr int ROPE_LAUNCH = 1 << 22;  // tokens of a launch: a grid's threads (here up to 2^30) have to stay below 2^32
 
 struct RopeParams {
   const uint16_t *q, *k, *v, *qw, *kw;
@@ -24,7 +25,7 @@ struct RopeParams {
   const int32_t *positions, *slots;
   uint16_t *q_out, *k_out, *k_cache, *v_cache;
   int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh, qo_st, qo_sh, ko_st, ko_sh, c_sp, c_st, c_sh;
-  int tokens, hq, hk, rotary, interleaved, page_shift;
+  int first, tokens, hq, hk, rotary, interleaved, page_shift;  // tokens first .. of all `tokens`, as many as the launch has
   int64_t n_slots;  // slots of the cache; 0: no cache
   float eps;
 };
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void qk_norm_rope_kernel(RopeParams p
   constexpr int L = D / 8, GROUPS = ROPE_THREADS / L;  // lanes of a row, rows at a time
   __shared__ float2 turn[TB][D / 2];                   // cos, sin of a token's pairs; (1, 0) where nothing is rotated
   const int tid = threadIdx.x, j = tid % L, group = tid / L;
-  const int t0 = blockIdx.x * TB, nt = min(TB, p.tokens - t0);
+  const int t0 = p.first + blockIdx.x * TB, nt = min(TB, p.tokens - t0);
   for (int x = tid; x < nt * (D / 2); x += ROPE_THREADS) {
     const int t = x / (D / 2), pair = x % (D / 2);
     float2 cs = {1.f, 0.f};
