@@ -55,18 +55,24 @@ struct CacheRequest {
   int joins_before;  // rows to join of the requests before it
 };
 
-// Walks the requests of a call forward, 64 at a time, one to a lane.  (Made anew for each item: kept, it would take registers from the
-// loops.)
+// How far a walk has come: requests, items, rows of partial results and rows to join (of chunked requests, all KV heads) before the
+// present 64 requests.
+struct CacheBefore {
+  int r0 = 0, items = 0, rows = 0, joins = 0;
+};
+// Walks the requests of a call forward, 64 at a time, one to a lane.  (Made anew for each item, from the place where the last one was:
+// kept whole, it would take registers from the loops, and begun at the first request each time, the lookups of a call would grow with
+// the square of its requests: 1024 of one token over up to 40, 8 KV heads, 89 us and 145, 65536 5.2 ms and 262.)
 template <int TILE>
-struct CacheWalk {
+struct CacheWalk : CacheBefore {
   const CacheAttnParams &p;
   const int lane;
-  // requests, items, rows of partial results and rows to join (of chunked requests, all KV heads) before the present 64
-  int r0 = 0, items = 0, rows = 0, joins = 0;
   int first, end, keys;  // of this lane's request, as the arrays hold them
   int upto, parts, joint;  // items, rows and rows to join up to and with it
   bool good;
-  __device__ __forceinline__ CacheWalk(const CacheAttnParams &params, int l) : p(reloaded(params)), lane(l) { look(); }
+  __device__ __forceinline__ CacheWalk(const CacheAttnParams &params, int l, const CacheBefore &from = {}) : CacheBefore(from), p(reloaded(params)), lane(l) {
+    look();
+  }
   __device__ __forceinline__ void look() {
     const int r = r0 + lane;
     const bool live = r < p.n_req;
@@ -100,8 +106,10 @@ struct CacheWalk {
       look();
     }
   }
-  __device__ __forceinline__ bool item(int index, CacheRequest &out) {
-    return seek([index](const CacheWalk &w) { return w.upto > index; }, out);
+  __device__ __forceinline__ bool item(int index, CacheRequest &out, CacheBefore &before) {
+    const bool found = seek([index](const CacheWalk &w) { return w.upto > index; }, out);
+    before = *this;
+    return found;
   }
   __device__ __forceinline__ bool join(int index, CacheRequest &out) {
     return seek([index](const CacheWalk &w) { return w.joint > index; }, out);
@@ -364,7 +372,8 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_narrow_kernel(CacheA
   const uint32_t v_lane = 2u * (uint32_t)((lane / VL) * (int)p.c_st + 8 * (lane % VL));
 
   CacheRequest rq;
-  for (int index = blockIdx.x; CacheWalk<ROWS>(p, lane).item(index, rq); index += gridDim.x) {
+  CacheBefore before;
+  for (int index = blockIdx.x; CacheWalk<ROWS>(p, lane, before).item(index, rq, before); index += gridDim.x) {
     const CacheItem it = item_of(rq, index, reloaded(p).hk);
     CacheRows<D, NC> rows;
     const int row0 = it.tile * ROWS;
@@ -660,7 +669,8 @@ __global__ __launch_bounds__(CA_THREADS, 2) void cache_attn_wide_kernel(CacheAtt
   auto slot_of = [](int s) { return (uint32_t)(s % RING) * (2 * TILE); };
 
   CacheRequest rq;
-  for (int index = blockIdx.x; CacheWalk<ROWS>(p, lane).item(index, rq); index += gridDim.x) {
+  CacheBefore before;
+  for (int index = blockIdx.x; CacheWalk<ROWS>(p, lane, before).item(index, rq, before); index += gridDim.x) {
     const CacheItem it = item_of(rq, index, reloaded(p).hk);
     CacheRows<D, NC> rows;
     const int row0 = it.tile * ROWS + w * WROWS;
