@@ -514,7 +514,8 @@ sp_status sp_cache_attn_workspace_bytes(const sp_step_shape *shape, const sp_cac
  * A row that sees no key (a refused request, pages that do not exist, an empty mask) gets o = 0 and lse = -inf.  Keys and values
  * that a row does not see do not touch it, whatever they hold (NaN and infinities among them).  Rows of o and lse behind
  * tok_start[n_requests] are left as they were.  A request with seq_len below its number of new tokens counts as refused.
- * Where tok_start falls, the rows of the requests from there on are unspecified; nothing outside them is touched.
+ * Requests are looked up 64 at a time: where tok_start[r + 1] < tok_start[r], the rows of the requests from r - r % 64 on are
+ * unspecified.  Those of the requests before are as ever, and nothing outside o and lse is touched.
  * A request's rows have the same bits whatever else the call holds, at which places its pages lie and however often it is made,
  * as long as max_new * n_q_heads / n_kv_heads stays on one side of 16 (1 to 16: kernel for few rows; more: for many).
  *   q           device bf16 [n_tokens][n_q_heads][head_dim] (strides as given)

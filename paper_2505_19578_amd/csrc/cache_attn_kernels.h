@@ -78,7 +78,7 @@ struct CacheWalk : CacheBefore {
     const bool live = r < p.n_req;
     first = live ? p.start[r] : 0, end = live ? p.start[r + 1] : 0, keys = live ? p.seq[r] : 0;
     const CacheShare s = cache_share(first, end, keys, p.n_tok, p.most_keys, p.group, TILE, p.hk, p.many_split);
-    good = !any_lane(end < first);  // otherwise this is no tok_start: nothing behind is done, so that no index leaves its buffer
+    good = !any_lane(end < first);  // otherwise this is no tok_start: nothing is done for these 64 and all behind, so that no index leaves its buffer
     upto = items + (int)wave_prefix((uint32_t)(s.tiles * p.hk * s.chunks));
     parts = rows + (int)wave_prefix((uint32_t)(s.chunks > 1 ? s.rows * p.hk * s.chunks : 0));
     joint = joins + (int)wave_prefix((uint32_t)(s.chunks > 1 ? s.rows * p.hk : 0));
