@@ -437,11 +437,13 @@ sp_status sp_cache_plan_workspace_bytes(int32_t n_requests, size_t *bytes);
  *              3).  Requests are served in order from the end of the list of free pages: the j-th page of all requests is
  *              free_pages[n_free - 1 - j]; a request for which they do not suffice gets none, and so does every later one
  *              that lacks any.  Fresh pages are appended to the request's row; other entries of block_table stay as they are.
- *   slots      of new token i of a request that is served: that of its position ctx_len + i; -1 for the tokens of refused
- *              requests and for rows behind the last token, so that a padded batch writes nothing
- *   positions  ctx_len + depth of the token in its tree (without parents: ctx_len + i); 0 where the slot is -1
+ *   slots      of new token i of a request that is served: that of its position ctx_len + i (-1 if its page's number is negative
+ *              or the slot's passes 32 bits); -1 for the tokens of refused requests and for rows behind the last token, so that a
+ *              padded batch writes nothing
+ *   positions  ctx_len + depth of the token in its tree (without parents: ctx_len + i), whatever page it lies on; 0 for the tokens
+ *              of refused requests and for rows behind the last token
  *   tree_mask  bit j % 64 of word j / 64: new token j is an ancestor of the token, or the token itself (without parents:
- *              all tokens up to it); 0 where the slot is -1
+ *              all tokens up to it); 0 for the tokens of refused requests and for rows behind the last token
  *   seq_len    ctx_len + new_len, or 0 for a refused request
  *   n_free     at most free_capacity and at least 0 of it counts; n_free_out is what is left of it
  *
