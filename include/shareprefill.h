@@ -513,8 +513,10 @@ sp_status sp_cache_attn_workspace_bytes(const sp_step_shape *shape, const sp_cac
  * of the context and those new tokens j whose bit is set in its tree_mask words (mask_words 0: j <= i); bits of tokens that
  * do not exist mean nothing.  Query head h reads KV head h / (n_q_heads / n_kv_heads).
  *   o = sum_s p_s v_s, p = softmax of scale * q.k over the keys that are seen;  lse = ln sum_s e^(scale * q.k_s)
- * A row that sees no key (a refused request, pages that do not exist, an empty mask) gets o = 0 and lse = -inf.  Keys and values
- * that a row does not see do not touch it, whatever they hold (NaN and infinities among them).  Rows of o and lse behind
+ * A row that sees no key (a refused request, pages that do not exist, an empty mask) gets o = 0 and lse = -inf, and so does one
+ * that sees only keys of score -infinity.  Keys and values that a row does not see do not touch it, whatever they hold (NaN and
+ * infinities among them).  Scores, and sums of values with weights of up to 2^8, are formed in 32 bits: a finite value whose part of
+ * them passes 2^128 (2^8 times the keys times |v|) counts as infinite.  Rows of o and lse behind
  * tok_start[n_requests] are left as they were.  A request with seq_len below its number of new tokens counts as refused.
  * Requests are looked up 64 at a time: where tok_start[r + 1] < tok_start[r], the rows of the requests from r - r % 64 on are
  * unspecified.  Those of the requests before are as ever, and nothing outside o and lse is touched.
@@ -523,7 +525,10 @@ sp_status sp_cache_attn_workspace_bytes(const sp_step_shape *shape, const sp_cac
  *   q           device bf16 [n_tokens][n_q_heads][head_dim] (strides as given)
  *   k_cache, v_cache, block_table, seq_len, tok_start, tree_mask  as sp_cache_plan and sp_qk_norm_rope leave them
  *   o           device bf16 (output; not q's memory);  lse: device fp32 [n_tokens][n_q_heads] or NULL (output)
- *   workspace   sp_cache_attn_workspace_bytes(shape, cache)
+ *   workspace   sp_cache_attn_workspace_bytes(shape, cache): partial results, for the longest requests that the table holds, as lengths
+ *               are not known on the host; about 4 (head_dim + 4) bytes per query row (token and head) and per chunk of a row of
+ *               the table, max_pages * page_size / 1024 chunks and at least 16 (none up to 256 keys).  256 requests of one token and 32
+ *               query heads of 128 with a table for 131072 keys: 558 MB.  A table no wider than the longest request keeps it small
  */
 sp_status sp_cache_attn(const sp_step_shape *shape, const sp_cache_shape *cache, const void *q, const void *k_cache,
                         const void *v_cache, const int32_t *block_table, const int32_t *seq_len, const int32_t *tok_start,

@@ -36,3 +36,17 @@ def test_an_infinite_value_far_below_the_largest_weight(hq, new, value, ctx):
         _check(s, got, d)
         assert (got[0][:, :, 11] == value).all() if value == value else np.isnan(got[0][:, :, 11]).all()
         assert np.isfinite(np.delete(got[0], 11, axis=2)).all()
+
+
+@pytest.mark.parametrize("hq,new", [(2, 1), (4, 10), (4, 60)])
+def test_a_row_of_scores_of_minus_infinity_alone(hq, new):
+    """An infinite query against keys of the other sign: every weight is e^-inf, and the row is as one that sees no key."""
+    s = _step([1500], [new], hq, 1, 64, 16, 0, 5)
+    s["k"][..., 3] = -s["k"][..., 3].abs() - 1
+    clean = _attend(s)
+    s["q"][0, 1, 3] = float("inf")
+    got = _attend(s)
+    assert (got[0][0, 1] == 0).all() and np.isneginf(got[1][0, 1])
+    for a, b in zip(got, clean):
+        a[0, 1] = b[0, 1]
+        assert np.array_equal(a, b)
