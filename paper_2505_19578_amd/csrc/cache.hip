@@ -108,7 +108,8 @@ size_t plan_bytes(int32_t n) { return ((size_t)2 * n + 1) * sizeof(int32_t); }
 // (one of 100K 99 and 97).  Two column groups to a wavefront, which read a key's fragment from LDS once for 32 rows instead of 16, from
 // 193 rows on: below, shorter steps of more workgroups are faster (us, one group and two: 12 contexts of up to 6150 with 147 rows 42
 // and 52, 8 of 4000 with 128 51 and 51 and with 192 70 and 83, 4 of 30000 with 147 84 and 118), above it turns (4 of 30000 with 224
-// rows 195 and 178, one of 131000 with 512 388 and 330; one of 8000 with 224 31 and 43).
+// rows 195 and 178, one of 131000 with 512 388 and 330), though not for a lone short one: of 8000 with 224 rows 31 and 43, the price of a rule by
+// the rows alone.
 int attn_tile_rows(const sp_step_shape *s, const sp_cache_shape *c) {
   const int64_t rows = (int64_t)s->max_new * (s->n_q_heads / c->n_kv_heads);
   return rows <= 16 ? 16 : rows <= 192 ? 64 : 128;

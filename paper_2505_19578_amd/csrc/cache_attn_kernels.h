@@ -605,10 +605,13 @@ __device__ __forceinline__ void wait_copies() {
 // Step s: the matrix pipe takes S of step s + 1, then O += V P of step s; beside it the vector unit makes the weights of step s,
 // then the largest of S of step s + 1.
 //
-// A tree of 64 tokens over 131000, 64 query heads: 331 us cold and 365 when repeated (the clock falls under the load) = 830 and 750
-// TFLOP/s next to 1184 of a large library product; the matrix pipe is busy 38 % of the cycles, the vector unit 46 %, and what is
-// left is their waiting for each other.  Twelve trees of 21 over up to 6150, 28 query heads: 45 us for 87 MB of keys and
-// values (36 with one column group): start and end of the workgroups, about 8 us, and 40 steps.
+// A tree of 64 tokens over 131000, 64 query heads: 328 to 359 us on different boxes (the clock falls under the load) = 840 to 766
+// TFLOP/s next to 1184 of a large library product; the matrix pipe is busy 37 % of the cycles, the vector unit 46 %, and what is
+// left is their waiting for each other and, after each pair's barrier, for three registers that come back from scratch: with two
+// column groups of 128 the kernel holds 256 and spills 56, most of them for the careful pass and the rare branches.  Twelve trees of 21
+// over up to 6150, 28 query heads (one column group, nothing spilled): 36 us for 87 MB of keys and values: start and end of the
+// workgroups, about 8 us, and 40 steps.  A tile walks every key of its chunk, in a chain also those behind its last token, which
+// it hides: a prompt over no context does twice the products that it needs.
 //
 // N products groups, group n with the fragment that read(n) names: use(n, fragment) issues it and its share of the vector work.
 // AHEAD fragments are on their way before the first group and one more goes out with each, in this order (the fences): left to

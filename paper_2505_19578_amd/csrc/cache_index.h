@@ -81,8 +81,9 @@ struct CacheShare {
 //   more             a KV head has work for many workgroups, and a chunk's own costs are small next to it: 256 / t chunks over all KV
 //                    heads (at least 16 / t a head), of at least t hk / 8 units.  Against the rule above, 32 query heads: one request
 //                    of 64 tokens over 8000 under 4 KV heads 43 us and 109, four 66 and 115, eight 130 and 134, sixteen 239 and 197;
-//                    of 56 tokens under 8 KV heads 45 and 66, 70 and 79, 135 and 123, 258 and 234.  (From 65 rows on: 12 requests of 21
-//                    tokens over 6150, 28 query and 4 KV heads, 90 and 73, one 33 and 45.)
+//                    of 56 tokens under 8 KV heads 45 and 66, 70 and 79, 135 and 123, 258 and 234.  Batches that fill
+//                    the chip lose, most where contexts are short: sixteen of 64 tokens over 1200 under 4 KV heads 88 and 57.  (From 65
+//                    rows on: 12 requests of 21 tokens over 6150, 28 query and 4 KV heads, 90 and 73, one 33 and 45.)
 constexpr uint32_t CACHE_FEW_SPLIT = 16;
 constexpr int32_t cache_many_split(int32_t hk) { return 256 / hk > (int32_t)CACHE_FEW_SPLIT ? 256 / hk : (int32_t)CACHE_FEW_SPLIT; }
 constexpr uint32_t cache_chunk_units(uint32_t units, uint32_t rows, uint32_t hk, uint32_t many_split) {
