@@ -605,7 +605,7 @@ __device__ __forceinline__ void wait_copies() {
 // Step s: the matrix pipe takes S of step s + 1, then O += V P of step s; beside it the vector unit makes the weights of step s,
 // then the largest of S of step s + 1.
 //
-// A tree of 64 tokens over 131000, 64 query heads: 328 to 359 us on different boxes (the clock falls under the load) = 840 to 766
+// A tree of 64 tokens over 131000, 64 query heads: 328 to 359 us on different cards (the clock falls under the load) = 840 to 766
 // TFLOP/s next to 1184 of a large library product; the matrix pipe is busy 37 % of the cycles, the vector unit 46 %, and what is
 // left is their waiting for each other and, after each pair's barrier, for three registers that come back from scratch: with two
 // column groups of 128 the kernel holds 256 and spills 56, most of them for the careful pass and the rare branches.  Twelve trees of 21
